@@ -3,17 +3,19 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "liblaplace_nystrom.so")
+OBJ_DIR = os.path.join(LIB_DIR, "obj")
 ROOT = os.path.dirname(HERE)
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
+    "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
 ]
 
 
@@ -21,22 +23,49 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def _depends(path: str, seen=None):
+    """The file and every file it includes by a quoted path, directly or through another."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path not in seen and os.path.exists(path):
+        seen.add(path)
+        with open(path) as f:
+            for inc in re.findall(r'^\s*#include\s+"([^"]+)"', f.read(), re.M):
+                _depends(os.path.join(os.path.dirname(path), inc), seen)
+    return seen
+
+
+def _newest(paths) -> float:
+    return max(os.path.getmtime(p) for p in paths)
+
+
 def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
-    t = os.path.getmtime(LIB)
-    deps = glob.glob(os.path.join(CSRC, "*")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
-    return any(os.path.getmtime(f) > t for f in deps)
+    return any(_newest(_depends(s)) > os.path.getmtime(LIB) for s in sources())
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/*.cu into lib/liblaplace_nystrom.so if anything changed."""
-    if force or _stale():
-        os.makedirs(LIB_DIR, exist_ok=True)
-        tmp = LIB + f".tmp{os.getpid()}"
-        cmd = ["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + sources()
-        subprocess.check_call(cmd)
-        os.replace(tmp, LIB)
+    """Compile csrc/*.cu (side by side, each only if it or a file it includes changed) and link them into
+    lib/liblaplace_nystrom.so."""
+    if not (force or _stale()):
+        return LIB
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    tag = f".tmp{os.getpid()}"
+    objects, running = [], []
+    for src in sources():
+        obj = os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o")
+        objects.append(obj)
+        if force or not os.path.exists(obj) or _newest(_depends(src)) > os.path.getmtime(obj):
+            cmd = ["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj + tag, src]
+            running.append((subprocess.Popen(cmd), cmd, obj))
+    failed = [cmd for proc, cmd, _ in running if proc.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(1, failed[0])
+    for _, _, obj in running:
+        os.replace(obj + tag, obj)
+    subprocess.check_call(["nvcc"] + NVCC_FLAGS + ["-shared", "-o", LIB + tag] + objects)
+    os.replace(LIB + tag, LIB)
     return LIB
 
 
