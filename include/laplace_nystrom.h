@@ -296,6 +296,90 @@ int landmarks_pool_bwd(const ln_problem* p, const float* dL, void* dK, void* str
 int laplace_nystrom_saved_array(const ln_problem* p, const char* name, int64_t info[5]);
 
 /*
+ * Preparation of queries and keys, and the softmax attention that stands beside the Laplacian one (Eq. 1-2 is what the paper
+ * replaces; a model may keep it in some layers).  Tensors of these entry points are views: [B, H, n, d] with the d channels of
+ * a row adjacent and any strides of batch, head and token, in elements, that are multiples of 16 bytes (slices of a
+ * projection's [B, n, heads, d] output, or of a cache); `data` is 16-byte aligned.  The stride of an axis of length one is not
+ * looked at.  An input's stride may be zero (a broadcast axis); the rows of an output must be distinct (LN_ERR_ARG).  Both views
+ * of a call are on the device that is current.  Sizes are positive (LN_ERR_ARG); more than 2^30 tokens an axis or 2^31 - 64
+ * rows of a call are LN_ERR_UNSUPPORTED.
+ */
+typedef struct ln_view { void* data; int64_t batch, head, token; } ln_view;
+
+/*
+ * Rotary positions.  The channel pairs (2i, 2i+1) (interleaved) or (i, i + r/2) (half layout) of the first r channels turn by
+ * 2 pi pos turns_i and are scaled by `factor`; the other channels are copied.  turns_i is given as a 64-bit binary fraction of a
+ * turn, floor(2^64 frac(angle per position / 2 pi)), so that the angle of a far position keeps its digits.
+ */
+typedef struct ln_rope {
+  int32_t d, r;              /* head dim 32, 64 or 128; rotated channels, 0 <= r <= d, a multiple of 16 (LN_ERR_UNSUPPORTED) */
+  int32_t interleaved;       /* 1: pairs (2i, 2i+1);  0: pairs (i, i + r/2)                                    */
+  int32_t dtype;             /* ln_dtype of every view of the call                                             */
+  const uint64_t* turns;     /* device [r/2] (NULL iff r == 0)                                                 */
+  float factor;              /* finite                                                                         */
+  const int32_t* pos;        /* device, position of (b, token) at pos[b pos_batch + token pos_token], any sign, */
+  int64_t pos_batch, pos_token; /* or NULL: start + token                                                      */
+  int32_t start;
+} ln_rope;
+
+/*
+ * Qr = rope(Q), Kr = rope(K) in one launch; Hk == 0: no K.  rope_bwd applies the transpose to the gradients of Qr and Kr (with
+ * the same positions and factor), which is the whole backward pass.  An output may be its own input (same view), else
+ * they must not overlap.
+ */
+int rope_fwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, const ln_view* Q, const ln_view* K,
+             const ln_view* Qr, const ln_view* Kr, void* stream);
+int rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, const ln_view* dQr, const ln_view* dKr,
+             const ln_view* dQ, const ln_view* dK, void* stream);
+
+/*
+ * RMS norm of every query and key head and the rotation in one pass: Qr = rope(gq o Q rstd), rstd = (mean_c Q_c^2 + eps)^-1/2 per
+ * row, and the same for K with gk.  gq, gk: device fp32 [d], 16-byte aligned, or NULL = ones; r == 0: the norm alone.  The
+ * backward pass recomputes rstd from Q and K; dgq, dgk (fp32 [d], or NULL) are summed over batch, heads and tokens in a fixed
+ * order.  Outputs may be their own inputs as in rope_fwd (dQ over dQr or over Q).
+ */
+int qk_norm_rope_fwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, float eps, const float* gq, const float* gk,
+                     const ln_view* Q, const ln_view* K, const ln_view* Qr, const ln_view* Kr, void* stream);
+size_t qk_norm_rope_bwd_workspace_bytes(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk);
+int qk_norm_rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, float eps, const float* gq, const float* gk,
+                     const ln_view* Q, const ln_view* K, const ln_view* dQr, const ln_view* dKr, const ln_view* dQ,
+                     const ln_view* dK, float* dgq, float* dgk, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Softmax attention.  s_ij = scale q_i . k_j; with a cap, s = cap tanh(s / cap); with slopes, s -= slope_h |p_i - j|; the pairs
+ * that the masks leave are normalised over j, O_i = sum_j softmax_ij v_j, and lse_i = log sum_j exp(s_ij).  Query i stands at key
+ * position p_i = i + len - nq, where len = kv_len[b] (clamped to 0 .. nk) or nk: the last query stands at the last key.
+ * A pair is left if j < len, and (causal) j <= p_i or j < prefix[b], and (documents) doc_q[i] == doc_k[j] >= 0.
+ * A row with no pair left gets O = 0 and lse = -infinity, and no gradient.  Keys at or behind len, and keys and queries with a
+ * negative document (padding), may hold anything, infinities and NaN included: they are never multiplied.  Other masked pairs
+ * are left out of every sum, but share matrix products with pairs that are not: their values have to be finite.
+ */
+typedef struct ln_softmax {
+  int32_t B, Hq, Hk, nq, nk; /* Hk divides Hq: query head h reads key head h / (Hq / Hk)                       */
+  int32_t d, dtype;          /* d in {32, 64, 128}; B Hq <= 65535 (LN_ERR_UNSUPPORTED)                          */
+  float scale, cap;          /* scale > 0, finite; cap > 0, finite, or 0: none                                  */
+  int32_t causal;
+  const int32_t* prefix;     /* device [B] or NULL; needs causal (LN_ERR_ARG)                                  */
+  const int32_t* kv_len;     /* device [B] or NULL                                                             */
+  const float* slopes;       /* device [Hq] or NULL; a constant: no gradient                                   */
+  const int32_t* doc_q;      /* device [B, nq] and [B, nk], in any order, or both NULL.  A tile of keys whose    */
+  const int32_t* doc_k;      /* documents a tile of queries cannot meet is not read where documents are sorted */
+} ln_softmax;
+
+/*
+ * ws: scratch of softmax_attention_workspace_bytes(p, backward) bytes, undefined between calls; calls that may overlap on the
+ * GPU (two streams, two graphs) need one each.  lse: fp32 [B, Hq, nq], contiguous, written by the forward pass and read
+ * with O by the backward pass.  dev_status: NULL or int32 [B * Hq], zeroed by the call; bit 1: a wait inside a kernel ran out.
+ * dK and dV are sums over the query heads of a key head; rows of dK and dV at or behind len are zero.
+ */
+size_t softmax_attention_workspace_bytes(const ln_softmax* p, int32_t backward);
+int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, float* lse,
+                          void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O,
+                          const float* lse, const ln_view* dO, const ln_view* dQ, const ln_view* dK, const ln_view* dV, void* ws,
+                          size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/*
  * Self-test of failure detection (the paper has no counterpart).  Launches one tiny kernel that waits, with the
  * library's bounded wait and a limit of `probes` polls, on a barrier nothing ever arrives on; the wait gives up and
  * the kernel ORs bit 1 into dev_status[0] (device int32, not cleared by this call) and returns normally.  Shows a

@@ -10,6 +10,8 @@ from .binding import (  # noqa: F401
     laplace_nystrom_bwd, laplace_nystrom_fwd, laplace_nystrom_saved_bytes, laplace_nystrom_workspace_bytes,
     ns_pinv, ns_pinv_bwd, ns_pinv_static, trace_begin, trace_end, HostStep, laplace_nystrom_fwd_bwd_host,
     set_overlap, set_fused_sign, laplace_exact_fwd, Block, laplace_attention_block_fwd, laplace_attention_block_bwd, launch_count, laplace_nystrom_whiten_stats, saved_array, selftest_wait_timeout, fp32_add_probe,
+    Rope, rope_frequencies, rope_fwd, rope_bwd, qk_norm_rope_fwd, qk_norm_rope_bwd, SoftmaxAttention,
+    softmax_attention_workspace_bytes, softmax_attention_fwd, softmax_attention_bwd,
 )
 
 

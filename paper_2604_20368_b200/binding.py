@@ -6,16 +6,20 @@ loaded, or a tensor is not on a CUDA device, the call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import math
 import os
 from dataclasses import dataclass, field
 from typing import Optional
 
+import numpy as np
 import torch
 
 from . import build as _build
 
 LN_F32, LN_BF16 = 0, 1
+_TWO_PI = 2 * np.longdouble("3.14159265358979323846264338327950288")
 _STATUS = {0: "ok", -1: "invalid argument", -2: "outside the supported envelope",
            -3: "workspace too small", -4: "CUDA launch failed",
            -5: "problem exceeds the static scratch of the no-allocation entry point"}
@@ -29,6 +33,8 @@ EXPORTS = [
     "laplace_nystrom_whiten_stats_workspace_bytes", "laplace_nystrom_whiten_stats",
     "laplace_nystrom_saved_array", "ln_set_fused_sign", "laplace_attention_block_saved_bytes",
     "laplace_attention_block_workspace_bytes", "laplace_attention_block_fwd", "laplace_attention_block_bwd", "laplace_exact_fwd", "ln_selftest_wait_timeout", "ln_fp32_add_probe", "ln_fp32_add_probe_lane_ops",
+    "rope_fwd", "rope_bwd", "qk_norm_rope_fwd", "qk_norm_rope_bwd_workspace_bytes", "qk_norm_rope_bwd",
+    "softmax_attention_workspace_bytes", "softmax_attention_fwd", "softmax_attention_bwd",
 ]
 
 
@@ -172,6 +178,16 @@ def lib():
         L.laplace_attention_block_workspace_bytes.argtypes = [pp, pb]
         L.laplace_attention_block_fwd.argtypes = [pp, pb, vp, vp, vp, vp, vp, vp, sz, vp, vp]
         L.laplace_attention_block_bwd.argtypes = [pp, pb, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+        pr, pv, ps = ctypes.POINTER(_CRope), ctypes.POINTER(_CView), ctypes.POINTER(_CSoftmax)
+        L.rope_fwd.argtypes = L.rope_bwd.argtypes = [pr, i32, i32, i32, i32, pv, pv, pv, pv, vp]
+        L.qk_norm_rope_fwd.argtypes = [pr, i32, i32, i32, i32, f32, vp, vp, pv, pv, pv, pv, vp]
+        L.qk_norm_rope_bwd_workspace_bytes.restype = sz
+        L.qk_norm_rope_bwd_workspace_bytes.argtypes = [pr, i32, i32, i32, i32]
+        L.qk_norm_rope_bwd.argtypes = [pr, i32, i32, i32, i32, f32, vp, vp, pv, pv, pv, pv, pv, pv, vp, vp, vp, sz, vp]
+        L.softmax_attention_workspace_bytes.restype = sz
+        L.softmax_attention_workspace_bytes.argtypes = [ps, i32]
+        L.softmax_attention_fwd.argtypes = [ps, pv, pv, pv, pv, vp, vp, sz, vp, vp]
+        L.softmax_attention_bwd.argtypes = [ps, pv, pv, pv, pv, vp, pv, pv, pv, pv, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -463,6 +479,275 @@ def fp32_add_probe(blocks: int, iters: int, mode: int, sink: torch.Tensor, strea
 def launch_count() -> int:
     """Kernels the library has launched in this process so far."""
     return int(lib().ln_launch_count())
+
+
+# ------------------------------------------------------------------------------------------ rotary positions, head norms
+class _CView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class _CRope(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("r", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("turns", ctypes.c_void_p), ("factor", ctypes.c_float), ("pos", ctypes.c_void_p),
+                ("pos_batch", ctypes.c_int64), ("pos_token", ctypes.c_int64), ("start", ctypes.c_int32)]
+
+
+class _CSoftmax(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("nq", ctypes.c_int32),
+                ("nk", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float), ("causal", ctypes.c_int32), ("prefix", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("slopes", ctypes.c_void_p), ("doc_q", ctypes.c_void_p), ("doc_k", ctypes.c_void_p)]
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The tensors' device as the current one, and `stream` (or that device's current stream) as the stream of the call, its
+    allocations included."""
+    if device.type != "cuda":
+        raise ValueError("tensor must live on a CUDA device (there is no CPU path)")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream of {stream.device} for tensors on {device}")
+    with torch.cuda.device(device):
+        if stream is None:
+            yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        else:
+            with torch.cuda.stream(stream):
+                yield ctypes.c_void_p(stream.cuda_stream)
+
+
+def _heads(name, t, like, shape):
+    """Checks one [B, H, n, d] tensor and returns its view for the C ABI."""
+    if t.dim() != 4 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}: the channels of a row must be adjacent")
+    return _CView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _vector(name, t, dtype, shape, device):
+    """Checks an optional contiguous tensor of the call and returns its pointer."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected a contiguous {dtype} {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def rope_frequencies(r: int, base: float = 10000.0, scaling: Optional[dict] = None):
+    """Radians per position of the r / 2 channel pairs (fp64, CPU) and the factor on the rotated channels, for `Rope`.
+
+    base^(-2i/r), changed for sequences longer than the ones a model was trained on by one of
+      {"kind": "linear", "factor": s}      positions divided by s
+      {"kind": "ntk", "factor": s}         base multiplied by s^(r / (r - 2)): the slowest pair slows down by s, the fastest not
+      {"kind": "yarn", "factor": s, "original": n, "fast": 32, "slow": 1}   pairs that make more than `fast` turns over n tokens
+            stay, those with fewer than `slow` are divided by s, a ramp over the pair's index between; factor 0.1 ln s + 1
+      {"kind": "bands", "factor": s, "original": n, "high": 4, "low": 1}    the same with a ramp over the turns themselves
+    """
+    if r < 0 or r % 2 or base <= 0:
+        raise ValueError("r must be even and base positive")
+    i = torch.arange(r // 2, dtype=torch.float64)
+    f = base ** (-2 * i / max(r, 1))
+    if scaling is None:
+        return f, 1.0
+    kind, s = scaling["kind"], float(scaling["factor"])
+    if kind not in ("linear", "ntk", "yarn", "bands"):
+        raise ValueError(f"unknown scaling {kind!r}")
+    if not s >= 1:
+        raise ValueError("factor must be at least 1")
+    if kind in ("yarn", "bands") and not scaling.get("original", 0) > 0:
+        raise ValueError(f"{kind} needs the original length")
+    if kind == "linear":
+        return f / s, 1.0
+    if kind == "ntk":
+        return (base * s ** (r / (r - 2.0) if r > 2 else 1.0)) ** (-2 * i / max(r, 1)), 1.0
+    original = float(scaling["original"])
+    if kind == "yarn":
+        at = lambda turns: r * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))
+        lo = max(math.floor(at(float(scaling.get("fast", 32)))), 0)
+        hi = min(math.ceil(at(float(scaling.get("slow", 1)))), r - 1)
+        ramp = ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        return f / s * ramp + f * (1 - ramp), 0.1 * math.log(s) + 1.0
+    low, high = float(scaling.get("low", 1)), float(scaling.get("high", 4))
+    keep = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+    return f / s * (1 - keep) + f * keep, 1.0
+
+
+class Rope:
+    """Rotary positions of heads with d channels: `freq`, radians per position of the r / 2 channel pairs (a tensor or sequence of
+    doubles, or None: no rotation), the first r channels rotated, pairs (2i, 2i+1) if `interleaved` or (i, i + r/2); `factor`
+    scales the rotated channels.  Holds the table of the kernels on the device of `freq` (or `device`); make it once."""
+
+    def __init__(self, d: int, freq=None, interleaved: bool = False, factor: float = 1.0, device=None):
+        f = torch.zeros(0, dtype=torch.float64) if freq is None else torch.as_tensor(freq, dtype=torch.float64)
+        device = f.device if device is None else torch.device(device)
+        f = f.cpu().reshape(-1).numpy()
+        if not np.isfinite(f).all():
+            raise ValueError("freq must be finite")
+        self.d, self.r, self.interleaved, self.factor = int(d), 2 * f.size, bool(interleaved), float(factor)
+        # floor(2^64 frac(f / 2 pi)) in the 64-bit mantissa of x86's extended precision
+        part = f.astype(np.longdouble) / _TWO_PI % 1 * np.longdouble(2) ** 64
+        self.turns = torch.from_numpy(part.astype(np.uint64).view(np.int64)).to(device) if f.size else None
+
+    def c(self, like, B, n, pos, start) -> _CRope:
+        pb = pt = 0
+        if self.r and self.turns.device != like.device:
+            raise ValueError(f"Rope on {self.turns.device} for tensors on {like.device}")
+        if pos is not None:
+            if pos.dtype != torch.int32 or pos.device != like.device or pos.dim() not in (1, 2):
+                raise ValueError(f"pos: {pos.dtype} {tuple(pos.shape)} on {pos.device}, expected int32 [B, n] or [n] on {like.device}")
+            pos2 = pos[None] if pos.dim() == 1 else pos
+            if pos2.shape[1] != n or pos2.shape[0] not in (1, B):
+                raise ValueError(f"pos: shape {tuple(pos.shape)}, expected [{B}, {n}] or [{n}]")
+            pb, pt = (0 if pos2.shape[0] == 1 else pos2.stride(0)), pos2.stride(1)
+        return _CRope(self.d, self.r, int(self.interleaved), _dtype_code(like), None if not self.r else self.turns.data_ptr(),
+                      self.factor, None if pos is None else pos.data_ptr(), pb, pt, int(start))
+
+
+def _qk_outputs(Q, K, Qo, Ko):
+    """Outputs of the query / key preparation: contiguous unless given."""
+    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return (new(Q) if Qo is None else Qo), (None if K is None else new(K) if Ko is None else Ko)
+
+
+def _qk_shapes(rope, Q, K):
+    if Q.dim() != 4 or (K is not None and K.dim() != 4):
+        raise ValueError("Q and K must be [B, H, n, d]")
+    B, Hq, n, d = Q.shape
+    if d != rope.d:
+        raise ValueError(f"Rope of {rope.d} channels for heads of {d}")
+    Hk = 0 if K is None else K.shape[1]
+    return B, n, Hq, Hk, (B, Hq, n, d), (B, Hk, n, d)
+
+
+def _run_rope(entry, rope, Q, K, pos, start, Qo, Ko, stream):
+    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
+    with _on(Q.device, stream) as st:
+        Qo, Ko = _qk_outputs(Q, K, Qo, Ko)
+        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
+        cr = rope.c(Q, B, n, pos, start)
+        _check(getattr(lib(), entry)(ctypes.byref(cr), B, n, Hq, Hk, view("Q", Q, qs), view("K", K, ks), view("output of Q", Qo, qs),
+                                     view("output of K", Ko, ks), st), entry)
+    return Qo, Ko
+
+
+def rope_fwd(rope: Rope, Q, K=None, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
+    """Rotary positions on Q [B, Hq, n, d] and K [B, Hk, n, d] (or None) in one launch: returns Qr, Kr.  Token t of batch element b
+    stands at pos[b, t] (int32 [B, n] or [n]), or at start + t.  Any strides with adjacent channels; Qr = Q, Kr = K work in place."""
+    return _run_rope("rope_fwd", rope, Q, K, pos, start, Qr, Kr, stream)
+
+
+def rope_bwd(rope: Rope, dQr, dKr=None, pos=None, start: int = 0, dQ=None, dK=None, stream=None):
+    """Adjoint of rope_fwd: dQ, dK from the gradients of Qr and Kr (the transposed rotation; Q and K are not needed)."""
+    return _run_rope("rope_bwd", rope, dQr, dKr, pos, start, dQ, dK, stream)
+
+
+def qk_norm_rope_fwd(rope: Rope, Q, K, gq=None, gk=None, eps: float = 1e-6, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
+    """Qr = rope(gq * Q / rms(Q)), Kr = rope(gk * K / rms(K)), rms over the d channels of every head, in one pass.  gq, gk: fp32 [d]
+    or None; K may be None; positions, strides and outputs as in rope_fwd."""
+    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
+    with _on(Q.device, stream) as st:
+        Qr, Kr = _qk_outputs(Q, K, Qr, Kr)
+        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
+        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), Q.device)
+        cr = rope.c(Q, B, n, pos, start)
+        _check(lib().qk_norm_rope_fwd(ctypes.byref(cr), B, n, Hq, Hk, float(eps), gain("gq", gq), gain("gk", gk), view("Q", Q, qs),
+                                      view("K", K, ks), view("Qr", Qr, qs), view("Kr", Kr, ks), st), "qk_norm_rope_fwd")
+    return Qr, Kr
+
+
+def qk_norm_rope_bwd(rope: Rope, Q, K, dQr, dKr, gq=None, gk=None, eps: float = 1e-6, pos=None, start: int = 0, dQ=None, dK=None, stream=None):
+    """Adjoint of qk_norm_rope_fwd: dQ, dK, dgq, dgk (fp32 [d]; None where the gain, or K, is None).  Q and K are the inputs of the
+    forward call."""
+    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
+    with _on(Q.device, stream) as st:
+        dQ, dK = _qk_outputs(Q, K, dQ, dK)
+        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
+        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), Q.device)
+        cr = rope.c(Q, B, n, pos, start)
+        pq, pk = gain("gq", gq), gain("gk", gk)
+        dgq = None if gq is None else torch.empty_like(gq)
+        dgk = None if gk is None or K is None else torch.empty_like(gk)
+        ws = _bytes(lib().qk_norm_rope_bwd_workspace_bytes(ctypes.byref(cr), B, n, Hq, Hk), Q.device)
+        _check(lib().qk_norm_rope_bwd(ctypes.byref(cr), B, n, Hq, Hk, float(eps), pq, pk, view("Q", Q, qs), view("K", K, ks),
+                                      view("dQr", dQr, qs), view("dKr", dKr, ks), view("dQ", dQ, qs), view("dK", dK, ks),
+                                      _ptr(dgq), _ptr(dgk), _ptr(ws), ws.numel(), st), "qk_norm_rope_bwd")
+    return dQ, dK, dgq, dgk
+
+
+# ------------------------------------------------------------------------------------------ softmax attention
+@dataclass
+class SoftmaxAttention:
+    """Scores and masks of softmax attention of Q [B, Hq, nq, d] on K, V [B, Hk, nk, d] (Hk divides Hq).
+
+    scale: 1 / sqrt(d) if None.  cap: scores become cap tanh(s / cap) (0: not).  slopes: fp32 [Hq], slope_h |distance| is
+    subtracted (a constant, no gradient).  kv_len: int32 [B], keys behind it are not read; query i stands at position
+    i + kv_len - nq (or + nk - nq).  causal: keys up to the query's position, and those before prefix (int32 [B]).
+    doc_q, doc_k: int32 [B, nq], [B, nk]; a query sees the keys of its own document, a negative document is padding."""
+    scale: Optional[float] = None
+    cap: float = 0.0
+    causal: bool = False
+    prefix: Optional[torch.Tensor] = field(default=None, repr=False)
+    slopes: Optional[torch.Tensor] = field(default=None, repr=False)
+    doc_q: Optional[torch.Tensor] = field(default=None, repr=False)
+    doc_k: Optional[torch.Tensor] = field(default=None, repr=False)
+    kv_len: Optional[torch.Tensor] = field(default=None, repr=False)
+
+    def c(self, Q, K) -> _CSoftmax:
+        if Q.dim() != 4 or K.dim() != 4:
+            raise ValueError("Q and K must be [B, H, n, d]")
+        B, Hq, nq, d = Q.shape
+        Hk, nk = K.shape[1], K.shape[2]
+        whole = lambda name, t, s: _vector(name, t, torch.int32, s, Q.device)
+        return _CSoftmax(B, Hq, Hk, nq, nk, d, _dtype_code(Q), 1.0 / math.sqrt(d) if self.scale is None else float(self.scale),
+                         float(self.cap), int(bool(self.causal)), whole("prefix", self.prefix, (B,)), whole("kv_len", self.kv_len, (B,)),
+                         _vector("slopes", self.slopes, torch.float32, (Hq,), Q.device), whole("doc_q", self.doc_q, (B, nq)),
+                         whole("doc_k", self.doc_k, (B, nk)))
+
+
+def softmax_attention_workspace_bytes(sp: SoftmaxAttention, Q, K, backward: bool) -> int:
+    cs = sp.c(Q, K)
+    return int(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), int(backward)))
+
+
+def softmax_attention_fwd(sp: SoftmaxAttention, Q, K, V, O=None, lse=None, ws=None, dev_status=None, stream=None):
+    """O [B, Hq, nq, d] and lse fp32 [B, Hq, nq] (the logarithm of every row's sum; both are what the backward pass wants).  A row
+    that the masks leave empty gets O = 0, lse = -inf.  Any strides with adjacent channels.  ``ws``: a uint8 tensor of
+    softmax_attention_workspace_bytes(...), or None; calls that may overlap need one each."""
+    cs = sp.c(Q, K)
+    qs, ks = tuple(Q.shape), (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
+    with _on(Q.device, stream) as st:
+        if O is None:
+            O = torch.empty(qs, dtype=Q.dtype, device=Q.device)
+        if lse is None:
+            lse = torch.empty(qs[:3], dtype=torch.float32, device=Q.device)
+        if ws is None:
+            ws = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 0), Q.device)
+        view = lambda name, t, s: ctypes.byref(_heads(name, t, Q, s))
+        _check(lib().softmax_attention_fwd(ctypes.byref(cs), view("Q", Q, qs), view("K", K, ks), view("V", V, ks), view("O", O, qs),
+                                           _vector("lse", lse, torch.float32, qs[:3], Q.device), _ptr(ws), ws.numel(),
+                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), Q.device), st),
+               "softmax_attention_fwd")
+    return O, lse
+
+
+def softmax_attention_bwd(sp: SoftmaxAttention, Q, K, V, O, lse, dO, dQ=None, dK=None, dV=None, ws=None, dev_status=None, stream=None):
+    """Adjoint of softmax_attention_fwd: dQ, dK, dV.  O and lse are the forward call's."""
+    cs = sp.c(Q, K)
+    qs, ks = tuple(Q.shape), (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
+    with _on(Q.device, stream) as st:
+        new = lambda s: torch.empty(s, dtype=Q.dtype, device=Q.device)
+        dQ, dK, dV = new(qs) if dQ is None else dQ, new(ks) if dK is None else dK, new(ks) if dV is None else dV
+        if ws is None:
+            ws = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 1), Q.device)
+        view = lambda name, t, s: ctypes.byref(_heads(name, t, Q, s))
+        _check(lib().softmax_attention_bwd(ctypes.byref(cs), view("Q", Q, qs), view("K", K, ks), view("V", V, ks), view("O", O, qs),
+                                           _vector("lse", lse, torch.float32, qs[:3], Q.device), view("dO", dO, qs), view("dQ", dQ, qs),
+                                           view("dK", dK, ks), view("dV", dV, ks), _ptr(ws), ws.numel(),
+                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), Q.device), st),
+               "softmax_attention_bwd")
+    return dQ, dK, dV
 
 
 # ------------------------------------------------------------------------------------------ profiling aid

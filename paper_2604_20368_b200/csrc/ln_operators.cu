@@ -1,0 +1,262 @@
+// C ABI of the query / key preparation and of softmax attention: host-side validation, buffer layout and launches.
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/laplace_nystrom.h"
+#include "ln_host.cuh"
+#include "ln_rope.cuh"
+#include "ln_softmax_simt.cuh"
+
+using namespace ln;
+using namespace ln::host;
+
+namespace {
+
+constexpr long long kMostTokens = 1ll << 30, kMostRows = (1ll << 31) - 64;
+
+// Strides of the three outer axes as the kernels use them (an axis of length one has none); false if the view cannot be read
+// in 16-byte pieces, or if it is an output whose rows overlap.
+bool open_view(const ln_view* v, long long B, long long H, long long n, int d, int dtype, bool output, long long (&s)[3]) {
+  if (!v || !v->data || !aligned16(v->data)) return false;
+  const int per = dtype == LN_F32 ? 4 : 8;
+  const long long ext[3] = {B, H, n}, given[3] = {v->batch, v->head, v->token};
+  for (int i = 0; i < 3; ++i) {
+    s[i] = ext[i] == 1 ? 0 : given[i];
+    if (s[i] < 0 || s[i] % per || s[i] > (1ll << 38)) return false;
+  }
+  if (!output) return true;
+  int order[3] = {0, 1, 2};                         // by stride
+  for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < 2 - i; ++k)
+      if (s[order[k]] > s[order[k + 1]]) { const int t = order[k]; order[k] = order[k + 1]; order[k + 1] = t; }
+  long long span = d;                               // elements that the axes so far cover
+  for (int i = 0; i < 3; ++i) {
+    const int o = order[i];
+    if (ext[o] == 1) continue;
+    if (s[o] < span) return false;
+    span = s[o] * (ext[o] - 1) + span;
+  }
+  return true;
+}
+
+// ------------------------------------------------------------------------------------------ rotary positions, norms
+int check_rope(const ln_rope* p, int B, int n, int Hq, int Hk) {
+  if (!p || B <= 0 || n <= 0 || Hq <= 0 || Hk < 0 || p->d <= 0 || p->r < 0 || p->r > p->d) return LN_ERR_ARG;
+  if (p->dtype != LN_F32 && p->dtype != LN_BF16) return LN_ERR_ARG;
+  if ((p->r > 0) != (p->turns != nullptr) || !isfinite(p->factor)) return LN_ERR_ARG;
+  if (reinterpret_cast<uintptr_t>(p->turns) & 7u || reinterpret_cast<uintptr_t>(p->pos) & 3u) return LN_ERR_ARG;
+  if ((p->d != 32 && p->d != 64 && p->d != 128) || p->r % 16) return LN_ERR_UNSUPPORTED;
+  if (n > kMostTokens || (long long)B * n > kMostRows / ((long long)Hq + Hk)) return LN_ERR_UNSUPPORTED;
+  return LN_OK;
+}
+
+// Heads per lane group and CTAs.  Every lane group forms the sines of its token once for all its heads, so a group walks as
+// many heads as leave the GPU full.
+struct QkPlan { int hpg, chunks, ctas; };
+QkPlan plan_qk(const ln_rope* p, int B, int n, int heads, bool bwd) {
+  const int lpr = p->d / (p->dtype == LN_F32 ? 4 : 8), tpw = 32 / lpr;
+  const long long groups = ((long long)B * n + tpw - 1) / tpw, slots = 8ll * 6 * sm_count();       // warps resident at six CTAs per SM
+  int hpg = heads;
+  while (hpg > 1 && groups * ((heads + hpg - 1) / hpg) < slots) hpg = (hpg + 1) / 2;
+  QkPlan q;
+  q.hpg = hpg; q.chunks = (heads + hpg - 1) / hpg;
+  const long long want = (groups * q.chunks + 7) / 8, most = bwd ? 4ll * sm_count() : 24ll * sm_count();
+  q.ctas = (int)(want < most ? want : most);
+  return q;
+}
+
+int run_qk(const ln_rope* p, int mode, float sign, int B, int n, int Hq, int Hk, float eps, const float* gq, const float* gk,
+           const ln_view* Q, const ln_view* K, const ln_view* dQr, const ln_view* dKr, const ln_view* Qo, const ln_view* Ko,
+           float* dgq, float* dgk, float* part, cudaStream_t st) {
+  QkArgs a = {};
+  const ln_view *in[2] = {Q, K}, *up[2] = {dQr, dKr}, *out[2] = {Qo, Ko};
+  const float* g[2] = {gq, gk};
+  const int H[2] = {Hq, Hk};
+  for (int s = 0; s < 2; ++s) {
+    QkTensor& t = a.t[s];
+    t.H = H[s]; t.g = g[s];
+    if (!H[s]) continue;
+    if (!open_view(in[s], B, H[s], n, p->d, p->dtype, false, t.xs) || !open_view(out[s], B, H[s], n, p->d, p->dtype, true, t.ys)) return LN_ERR_ARG;
+    if (mode == QK_NORM_BWD && !open_view(up[s], B, H[s], n, p->d, p->dtype, false, t.ds)) return LN_ERR_ARG;
+    t.x = in[s]->data; t.y = out[s]->data; t.dy = mode == QK_NORM_BWD ? up[s]->data : nullptr;
+  }
+  const QkPlan q = plan_qk(p, B, n, Hq + Hk, mode == QK_NORM_BWD);
+  a.pos = p->pos; a.pos_b = p->pos_batch; a.pos_n = p->pos_token; a.start = p->start;
+  a.tokens = B * n; a.n = n; a.r = p->r; a.heads = Hq + Hk; a.hpg = q.hpg; a.chunks = q.chunks;
+  a.turns = reinterpret_cast<const unsigned long long*>(p->turns);
+  a.factor = p->factor; a.sign = sign; a.eps = eps; a.dgpart = part;
+  auto go = [&](auto type, auto lpr, auto inter) {
+    using T = decltype(type);
+    constexpr int L = decltype(lpr)::value;
+    constexpr bool I = decltype(inter)::value;
+    if (mode == QK_ROPE) LN_LAUNCH("k_rope_qk", st, enqueue(k_qk_rope<T, L, I, QK_ROPE>, q.ctas, 256, 0, st, a));
+    else if (mode == QK_NORM) LN_LAUNCH("k_qk_norm_rope", st, enqueue(k_qk_rope<T, L, I, QK_NORM>, q.ctas, 256, 0, st, a));
+    else LN_LAUNCH("k_qk_norm_rope_bwd", st, enqueue(k_qk_rope<T, L, I, QK_NORM_BWD>, q.ctas, 256, 0, st, a));
+  };
+  auto lanes = [&](auto type, auto inter) {
+    switch (p->d / Piece<decltype(type)>::E) {
+      case 4: go(type, std::integral_constant<int, 4>(), inter); break;
+      case 8: go(type, std::integral_constant<int, 8>(), inter); break;
+      case 16: go(type, std::integral_constant<int, 16>(), inter); break;
+      default: go(type, std::integral_constant<int, 32>(), inter); break;
+    }
+  };
+  auto layout = [&](auto type) { if (p->interleaved) lanes(type, std::true_type()); else lanes(type, std::false_type()); };
+  if (p->dtype == LN_F32) layout(float()); else layout(bf16());
+  if (part) LN_LAUNCH("k_gain_sum", st, enqueue(k_gain_sum, 2 * p->d / 32, 256, 0, st, part, q.ctas, p->d, dgq, dgk));
+  return launch_ok();
+}
+
+// ------------------------------------------------------------------------------------------ softmax attention
+int check_softmax(const ln_softmax* p) {
+  if (!p || p->B <= 0 || p->Hq <= 0 || p->Hk <= 0 || p->nq <= 0 || p->nk <= 0 || p->d <= 0 || p->Hq % p->Hk) return LN_ERR_ARG;
+  if (p->dtype != LN_F32 && p->dtype != LN_BF16) return LN_ERR_ARG;
+  if (!(p->scale > 0.f) || !isfinite(p->scale) || !(p->cap >= 0.f) || !isfinite(p->cap) || (p->causal != 0 && p->causal != 1)) return LN_ERR_ARG;
+  if ((p->prefix && !p->causal) || (p->doc_q != nullptr) != (p->doc_k != nullptr)) return LN_ERR_ARG;
+  const void* words[] = {p->prefix, p->kv_len, p->slopes, p->doc_q, p->doc_k};
+  for (const void* w : words)
+    if (reinterpret_cast<uintptr_t>(w) & 3u) return LN_ERR_ARG;
+  if ((p->d != 32 && p->d != 64 && p->d != 128) || (long long)p->B * p->Hq > 65535 || p->nq > kMostTokens || p->nk > kMostTokens) return LN_ERR_UNSUPPORTED;
+  return LN_OK;
+}
+
+// Workspace: the documents of every 64 tokens, and (backward) delta.
+struct SmWork { int4 *rq, *rk; float* delta; size_t bytes; };
+SmWork carve_softmax(const ln_softmax* p, bool bwd, void* base) {
+  Carver c(base);
+  SmWork w = {};
+  if (p->doc_q) {
+    w.rq = reinterpret_cast<int4*>(c.take((size_t)p->B * cdiv(p->nq, 64) * 4));
+    w.rk = reinterpret_cast<int4*>(c.take((size_t)p->B * cdiv(p->nk, 64) * 4));
+  }
+  if (bwd) w.delta = c.take((size_t)p->B * p->Hq * p->nq);
+  w.bytes = c.off;
+  return w;
+}
+
+SmArgs softmax_args(const ln_softmax* p, const SmWork& w, int32_t* dev_status) {
+  SmArgs a = {};
+  a.B = p->B; a.Hq = p->Hq; a.Hk = p->Hk; a.group = p->Hq / p->Hk; a.nq = p->nq; a.nk = p->nk; a.d = p->d;
+  a.scale = p->scale; a.cap = p->cap; a.causal = p->causal; a.prefix = p->prefix; a.kv_len = p->kv_len; a.slopes = p->slopes;
+  a.doc_q = p->doc_q; a.doc_k = p->doc_k; a.rq = w.rq; a.rk = w.rk; a.tq = (int)cdiv(p->nq, 64); a.tk = (int)cdiv(p->nk, 64);
+  a.delta = w.delta; a.dev_status = dev_status;
+  return a;
+}
+
+bool open_sm(const ln_softmax* p, const ln_view* v, bool keys, bool output, SmView* o) {
+  long long s[3];
+  if (!open_view(v, p->B, keys ? p->Hk : p->Hq, keys ? p->nk : p->nq, p->d, p->dtype, output, s)) return false;
+  o->p = v->data; o->b = s[0]; o->h = s[1]; o->t = s[2];
+  return true;
+}
+
+void softmax_docs(const SmArgs& a, const SmWork& w, cudaStream_t st) {
+  if (a.doc_q) LN_LAUNCH("k_sm_docs", st, enqueue(k_sm_docs, dim3(a.tq + a.tk, a.B), 32, 0, st, a.doc_q, a.doc_k, a.nq, a.nk, a.tq, a.tk, w.rq, w.rk));
+}
+
+template <typename T, int D> void softmax_fwd_simt(const SmArgs& a, cudaStream_t st) {
+  want_smem(k_softmax_fwd<T, D>, sm_fwd_smem<D>());
+  LN_LAUNCH("k_softmax_fwd", st, enqueue(k_softmax_fwd<T, D>, dim3(cdiv(a.nq, SS), a.B * a.Hq), 256, sm_fwd_smem<D>(), st, a));
+}
+template <typename T, int D> void softmax_bwd_simt(const SmArgs& a, cudaStream_t st) {
+  want_smem(k_softmax_bwd<T, D, false>, sm_bwd_smem<D, false>());
+  LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<T, D, false>, dim3(cdiv(a.nq, SS), a.B * a.Hq), 256, sm_bwd_smem<D, false>(), st, a));
+  want_smem(k_softmax_bwd<T, D, true>, sm_bwd_smem<D, true>());
+  LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<T, D, true>, dim3(cdiv(a.nk, SS), a.B * a.Hk), 256, sm_bwd_smem<D, true>(), st, a));
+}
+
+}  // namespace
+
+extern "C" {
+
+int rope_fwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, const ln_view* Q, const ln_view* K, const ln_view* Qr,
+             const ln_view* Kr, void* stream) {
+  const int rc = check_rope(p, B, n, Hq, Hk);
+  if (rc != LN_OK) return rc;
+  return run_qk(p, QK_ROPE, 1.f, B, n, Hq, Hk, 0.f, nullptr, nullptr, Q, K, nullptr, nullptr, Qr, Kr, nullptr, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+int rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, const ln_view* dQr, const ln_view* dKr, const ln_view* dQ,
+             const ln_view* dK, void* stream) {
+  const int rc = check_rope(p, B, n, Hq, Hk);
+  if (rc != LN_OK) return rc;
+  return run_qk(p, QK_ROPE, -1.f, B, n, Hq, Hk, 0.f, nullptr, nullptr, dQr, dKr, nullptr, nullptr, dQ, dK, nullptr, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+int qk_norm_rope_fwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, float eps, const float* gq, const float* gk,
+                     const ln_view* Q, const ln_view* K, const ln_view* Qr, const ln_view* Kr, void* stream) {
+  const int rc = check_rope(p, B, n, Hq, Hk);
+  if (rc != LN_OK) return rc;
+  if (!(eps >= 0.f) || !isfinite(eps) || !aligned16(gq) || !aligned16(gk)) return LN_ERR_ARG;
+  return run_qk(p, QK_NORM, 1.f, B, n, Hq, Hk, eps, gq, gk, Q, K, nullptr, nullptr, Qr, Kr, nullptr, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+size_t qk_norm_rope_bwd_workspace_bytes(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk) {
+  if (check_rope(p, B, n, Hq, Hk) != LN_OK) return 0;
+  return align_up((size_t)plan_qk(p, B, n, Hq + Hk, true).ctas * 2 * p->d * sizeof(float), 256);
+}
+
+int qk_norm_rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t Hk, float eps, const float* gq, const float* gk,
+                     const ln_view* Q, const ln_view* K, const ln_view* dQr, const ln_view* dKr, const ln_view* dQ, const ln_view* dK,
+                     float* dgq, float* dgk, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_rope(p, B, n, Hq, Hk);
+  if (rc != LN_OK) return rc;
+  if (!(eps >= 0.f) || !isfinite(eps) || !aligned16(gq) || !aligned16(gk) || !aligned16(dgq) || !aligned16(dgk)) return LN_ERR_ARG;
+  const bool gains = dgq || dgk;
+  if (gains && (!ws || !aligned16(ws))) return LN_ERR_ARG;
+  if (gains && ws_bytes < qk_norm_rope_bwd_workspace_bytes(p, B, n, Hq, Hk)) return LN_ERR_WORKSPACE;
+  return run_qk(p, QK_NORM_BWD, -1.f, B, n, Hq, Hk, eps, gq, gk, Q, K, dQr, dKr, dQ, dK, dgq, dgk, gains ? static_cast<float*>(ws) : nullptr,
+                static_cast<cudaStream_t>(stream));
+}
+
+size_t softmax_attention_workspace_bytes(const ln_softmax* p, int32_t backward) {
+  if (check_softmax(p) != LN_OK) return 0;
+  const size_t n = carve_softmax(p, backward != 0, nullptr).bytes;
+  return n ? n : 256;                               // never 0 for a valid problem
+}
+
+int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, float* lse, void* ws,
+                          size_t ws_bytes, int32_t* dev_status, void* stream) {
+  const int rc = check_softmax(p);
+  if (rc != LN_OK) return rc;
+  const SmWork w = carve_softmax(p, false, ws);
+  SmArgs a = softmax_args(p, w, dev_status);
+  if (!open_sm(p, Q, false, false, &a.q) || !open_sm(p, K, true, false, &a.k) || !open_sm(p, V, true, false, &a.v) || !open_sm(p, O, false, true, &a.o)) return LN_ERR_ARG;
+  if (!lse || !aligned16(lse) || !ws || !aligned16(ws)) return LN_ERR_ARG;
+  if (ws_bytes < w.bytes) return LN_ERR_WORKSPACE;
+  a.lse = lse;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dev_status) cudaMemsetAsync(dev_status, 0, sizeof(int32_t) * (size_t)p->B * p->Hq, st);
+  softmax_docs(a, w, st);
+  auto go = [&](auto type) {
+    using T = decltype(type);
+    if (p->d == 32) softmax_fwd_simt<T, 32>(a, st); else if (p->d == 64) softmax_fwd_simt<T, 64>(a, st); else softmax_fwd_simt<T, 128>(a, st);
+  };
+  if (p->dtype == LN_F32) go(float()); else go(bf16());
+  return launch_ok();
+}
+
+int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, const float* lse,
+                          const ln_view* dO, const ln_view* dQ, const ln_view* dK, const ln_view* dV, void* ws, size_t ws_bytes, int32_t* dev_status,
+                          void* stream) {
+  const int rc = check_softmax(p);
+  if (rc != LN_OK) return rc;
+  const SmWork w = carve_softmax(p, true, ws);
+  SmArgs a = softmax_args(p, w, dev_status);
+  if (!open_sm(p, Q, false, false, &a.q) || !open_sm(p, K, true, false, &a.k) || !open_sm(p, V, true, false, &a.v) || !open_sm(p, O, false, false, &a.o) ||
+      !open_sm(p, dO, false, false, &a.dout) || !open_sm(p, dQ, false, true, &a.dq) || !open_sm(p, dK, true, true, &a.dk) || !open_sm(p, dV, true, true, &a.dv)) return LN_ERR_ARG;
+  if (!lse || !aligned16(lse) || !ws || !aligned16(ws)) return LN_ERR_ARG;
+  if (ws_bytes < w.bytes) return LN_ERR_WORKSPACE;
+  a.lse = const_cast<float*>(lse);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dev_status) cudaMemsetAsync(dev_status, 0, sizeof(int32_t) * (size_t)p->B * p->Hq, st);
+  softmax_docs(a, w, st);
+  auto go = [&](auto type) {
+    using T = decltype(type);
+    if (p->d == 32) softmax_bwd_simt<T, 32>(a, st); else if (p->d == 64) softmax_bwd_simt<T, 64>(a, st); else softmax_bwd_simt<T, 128>(a, st);
+  };
+  if (p->dtype == LN_F32) go(float()); else go(bf16());
+  return launch_ok();
+}
+
+}  // extern "C"
