@@ -300,7 +300,8 @@ int laplace_nystrom_saved_array(const ln_problem* p, const char* name, int64_t i
  * replaces; a model may keep it in some layers).  Tensors of these entry points are views: [B, H, n, d] with the d channels of
  * a row adjacent and any strides of batch, head and token, in elements, that are multiples of 16 bytes (slices of a
  * projection's [B, n, heads, d] output, or of a cache); `data` is 16-byte aligned.  The stride of an axis of length one is not
- * looked at.  An input's stride may be zero (a broadcast axis); the rows of an output must be distinct (LN_ERR_ARG).  Both views
+ * looked at.  An input's stride may be zero (a broadcast axis; not the token axis of the softmax entry points, LN_ERR_ARG); the rows of an
+ * output must be distinct (LN_ERR_ARG).  Both views
  * of a call are on the device that is current.  Sizes are positive (LN_ERR_ARG); more than 2^30 tokens an axis or 2^31 - 64
  * rows of a call are LN_ERR_UNSUPPORTED.
  */

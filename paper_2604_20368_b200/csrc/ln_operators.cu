@@ -1,4 +1,5 @@
 // C ABI of the query / key preparation and of softmax attention: host-side validation, buffer layout and launches.
+#include <cudaTypedefs.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -6,6 +7,8 @@
 #include "ln_host.cuh"
 #include "ln_rope.cuh"
 #include "ln_softmax_simt.cuh"
+#include "ln_softmax_bwd_umma.cuh"
+#include "ln_softmax_umma.cuh"
 
 using namespace ln;
 using namespace ln::host;
@@ -147,7 +150,7 @@ bool open_sm(const ln_softmax* p, const ln_view* v, bool keys, bool output, SmVi
   long long s[3];
   if (!open_view(v, p->B, keys ? p->Hk : p->Hq, keys ? p->nk : p->nq, p->d, p->dtype, output, s)) return false;
   o->p = v->data; o->b = s[0]; o->h = s[1]; o->t = s[2];
-  return true;
+  return s[2] || (keys ? p->nk : p->nq) == 1;       // a broadcast token axis has no tensor map
 }
 
 void softmax_docs(const SmArgs& a, const SmWork& w, cudaStream_t st) {
@@ -163,6 +166,64 @@ template <typename T, int D> void softmax_bwd_simt(const SmArgs& a, cudaStream_t
   LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<T, D, false>, dim3(cdiv(a.nq, SS), a.B * a.Hq), 256, sm_bwd_smem<D, false>(), st, a));
   want_smem(k_softmax_bwd<T, D, true>, sm_bwd_smem<D, true>());
   LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<T, D, true>, dim3(cdiv(a.nk, SS), a.B * a.Hk), 256, sm_bwd_smem<D, true>(), st, a));
+}
+
+// The driver's encoder of tensor maps, by name (the library is not linked against the driver).
+PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+    cudaGetLastError();
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+  }();
+  return fn;
+}
+
+// Tensor map of a bf16 [B, H, n, d] view for blocks of `rows` rows x 64 channels; channels behind d and rows behind n arrive as zeros.
+bool tile_map(const SmView& v, int B, int H, int n, int d, int rows, TileMap* m) {
+  const auto encode = map_encoder();
+  if (!encode) return false;
+  m->head = v.h != 0; m->batch = v.b != 0;
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)n, (cuuint64_t)(m->head ? H : 1), (cuuint64_t)(m->batch ? B : 1)};
+  // a stride of zero: an axis of length one, or one that the map leaves out
+  const cuuint64_t strides[3] = {(cuuint64_t)(v.t ? 2 * v.t : 16), (cuuint64_t)(v.h ? 2 * v.h : 16), (cuuint64_t)(v.b ? 2 * v.b : 16)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  return encode(&m->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.p, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D> int softmax_fwd_umma(const SmArgs& a, cudaStream_t st) {
+  TileMap q, k, v;
+  if (!tile_map(a.q, a.B, a.Hq, a.nq, a.d, 128, &q) || !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 128, &k) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 128, &v)) return LN_ERR_CUDA;
+  auto go = [&](auto kern) {
+    want_smem(kern, SuFwd<D>::kSmem);
+    LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(cdiv(a.nq, 256), a.B * a.Hq), SU_THREADS, SuFwd<D>::kSmem, st, a, q, k, v));
+  };
+  if (a.cap > 0.f) { if (a.slopes) go(k_softmax_fwd_umma<D, true, true>); else go(k_softmax_fwd_umma<D, true, false>); }
+  else { if (a.slopes) go(k_softmax_fwd_umma<D, false, true>); else go(k_softmax_fwd_umma<D, false, false>); }
+  return LN_OK;
+}
+
+template <int D> int softmax_bwd_umma(const SmArgs& a, cudaStream_t st) {
+  TileMap sq, sdo, sk, sv, mq, mdo, mk, mv;                                  // stationary tiles of 128 rows, moving ones of 64
+  if (!tile_map(a.q, a.B, a.Hq, a.nq, a.d, 128, &sq) || !tile_map(a.dout, a.B, a.Hq, a.nq, a.d, 128, &sdo) || !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 128, &sk) ||
+      !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 128, &sv) || !tile_map(a.q, a.B, a.Hq, a.nq, a.d, 64, &mq) || !tile_map(a.dout, a.B, a.Hq, a.nq, a.d, 64, &mdo) ||
+      !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 64, &mk) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 64, &mv)) return LN_ERR_CUDA;
+  auto go = [&](auto q, auto kv) {
+    want_smem(q, SuBwd<D>::kSmem);
+    LN_LAUNCH("k_softmax_bwd_q", st, enqueue(q, dim3(cdiv(a.nq, 128), a.B * a.Hq), SU_THREADS, SuBwd<D>::kSmem, st, a, sq, sdo, mk, mv));
+    want_smem(kv, SuBwd<D>::kSmem);
+    LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(cdiv(a.nk, 128), a.B * a.Hk), SU_THREADS, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
+  };
+  if (a.cap > 0.f) {
+    if (a.slopes) go(k_softmax_bwd_umma<D, true, true, false>, k_softmax_bwd_umma<D, true, true, true>);
+    else go(k_softmax_bwd_umma<D, true, false, false>, k_softmax_bwd_umma<D, true, false, true>);
+  } else {
+    if (a.slopes) go(k_softmax_bwd_umma<D, false, true, false>, k_softmax_bwd_umma<D, false, true, true>);
+    else go(k_softmax_bwd_umma<D, false, false, false>, k_softmax_bwd_umma<D, false, false, true>);
+  }
+  return LN_OK;
 }
 
 }  // namespace
@@ -228,12 +289,13 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dev_status) cudaMemsetAsync(dev_status, 0, sizeof(int32_t) * (size_t)p->B * p->Hq, st);
   softmax_docs(a, w, st);
-  auto go = [&](auto type) {
-    using T = decltype(type);
-    if (p->d == 32) softmax_fwd_simt<T, 32>(a, st); else if (p->d == 64) softmax_fwd_simt<T, 64>(a, st); else softmax_fwd_simt<T, 128>(a, st);
-  };
-  if (p->dtype == LN_F32) go(float()); else go(bf16());
-  return launch_ok();
+  int made = LN_OK;
+  if (p->dtype == LN_BF16) made = p->d == 128 ? softmax_fwd_umma<128>(a, st) : softmax_fwd_umma<64>(a, st);
+  else if (p->d == 32) softmax_fwd_simt<float, 32>(a, st);
+  else if (p->d == 64) softmax_fwd_simt<float, 64>(a, st);
+  else softmax_fwd_simt<float, 128>(a, st);
+  const int launched = launch_ok();
+  return made != LN_OK ? made : launched;
 }
 
 int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, const float* lse,
@@ -251,12 +313,13 @@ int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dev_status) cudaMemsetAsync(dev_status, 0, sizeof(int32_t) * (size_t)p->B * p->Hq, st);
   softmax_docs(a, w, st);
-  auto go = [&](auto type) {
-    using T = decltype(type);
-    if (p->d == 32) softmax_bwd_simt<T, 32>(a, st); else if (p->d == 64) softmax_bwd_simt<T, 64>(a, st); else softmax_bwd_simt<T, 128>(a, st);
-  };
-  if (p->dtype == LN_F32) go(float()); else go(bf16());
-  return launch_ok();
+  int made = LN_OK;
+  if (p->dtype == LN_BF16) made = p->d == 128 ? softmax_bwd_umma<128>(a, st) : softmax_bwd_umma<64>(a, st);
+  else if (p->d == 32) softmax_bwd_simt<float, 32>(a, st);
+  else if (p->d == 64) softmax_bwd_simt<float, 64>(a, st);
+  else softmax_bwd_simt<float, 128>(a, st);
+  const int launched = launch_ok();
+  return made != LN_OK ? made : launched;
 }
 
 }  // extern "C"

@@ -1,0 +1,297 @@
+// Softmax attention on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 storage, backward.
+//
+// One CTA = 128 stationary rows X of one head; the moving rows Y stream through shared memory in tiles of 64, copied by TMA.
+//   queries stationary (KEYS false):  X1 = Q, X2 = dO;  Y1 = K, Y2 = V;   dQ += ds Y1
+//   keys stationary    (KEYS true):   X1 = K, X2 = V;   Y1 = Q, Y2 = dO of every query head of the group;  dK += ds Y1, dV += A Y2
+// Per tile: S = X1 Y1^T and dP = X2 Y2^T (128 x 64, K = d, operands in shared memory), then A = exp2(x - lse) and
+// ds = A (dP - delta) (1 - tanh^2), both rounded to bf16 and written over S and dP in TMEM, from where they are the left operands
+// of the products into the accumulators (128 x d in TMEM).  S and dP are double-buffered: the tensor core forms those of the next
+// tile while this one's exponentials are formed.  Warps 0-7: warp w owns rows 32 (w % 4) .. and columns 32 (w / 4) ..; warp 8
+// copies, warp 9 issues the products.  `scale` is applied once, to the accumulators.
+// Two passes form S and dP twice (7 products a pair instead of 5): no atomics, and every sum has one order.
+// Bound by the tensor core's operand reads: with 64 columns a product reads 128 + 64 rows of shared memory for 128 x 64 results.
+#pragma once
+#include "ln_softmax_umma.cuh"
+
+namespace ln {
+
+template <int D> struct SuBwd {
+  static constexpr int kX = 128 * D * 2, kY = 64 * D * 2;         // bytes of a stationary and of a moving tile
+  static constexpr int kStages = 4;
+  static constexpr size_t kSmem = 1024 + 2 * (size_t)kX + 2 * (size_t)kY * kStages;
+};
+
+template <int D, bool CAP, bool BIAS, bool KEYS>
+__global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mx1,
+                                                                  const __grid_constant__ TileMap mx2, const __grid_constant__ TileMap my1,
+                                                                  const __grid_constant__ TileMap my2) {
+  pdl_wait();
+  constexpr int NS = SuBwd<D>::kStages, XB = SuBwd<D>::kX, YB = SuBwd<D>::kY;
+  extern __shared__ __align__(16) char su_smem[];
+  char* base = su_smem + ((1024u - (umma::s32(su_smem) & 1023u)) & 1023u);
+  char *sX = base, *sY = base + 2 * XB;                                      // X1, X2; per stage Y1, Y2
+  __shared__ unsigned long long x_full, y_full[NS], y_free[NS], y_raw, l_full[NS], s_full[2], p_ready[2], acc_full, spare;
+  __shared__ uint32_t tmem_slot;
+  __shared__ __align__(16) float sL[KEYS ? NS : 1][64], sD[KEYS ? NS : 1][64];
+  __shared__ float sDelta[KEYS ? 1 : 2][128];
+  __shared__ int sh[2];
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.y / H, hs = blockIdx.y % H;
+  const int s0 = (KEYS ? (int)blockIdx.x : (int)gridDim.x - 1 - (int)blockIdx.x) * 128;     // the longest causal rows first
+  const SmMask m(a, b);
+  const int2 range = sm_range<128, KEYS>(a, m, b, s0, sh);
+  const int nt = range.y - range.x, total = KEYS ? nt * a.group : nt;
+  if (tid == 0) {
+    umma::mbar_init(&x_full, 1); umma::mbar_init(&y_raw, 1); umma::mbar_init(&acc_full, 1); umma::mbar_init(&spare, 1);
+    for (int s = 0; s < NS; ++s) { umma::mbar_init(&y_full[s], 1); umma::mbar_init(&y_free[s], 1); umma::mbar_init(&l_full[s], 1); }
+    for (int t = 0; t < 2; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 8); }
+  }
+  if (warp == 9) umma::tmem_alloc(&tmem_slot, 512);
+  umma::fence_before_sync();
+  __syncthreads();
+  umma::fence_after_sync();
+  const uint32_t tm = tmem_slot;                                             // S, dP of buffer 0, of buffer 1 (64 columns each); accumulators
+  constexpr int ACC2 = 256, ACC1 = 256 + D;                                  // ds Y1;  A Y2
+  const int* dq = a.doc_q ? a.doc_q + (long long)b * a.nq : nullptr;
+  const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
+  const int first_head = KEYS ? hs * a.group : hs;                           // query head of the first moving tile
+  bool ok = true;
+
+  if (warp == 8) {                                                           // copies
+    const bool one = umma::elect_one();
+    if (total > 0 && one) {
+      umma::mbar_expect_tx(&x_full, 2 * XB);
+#pragma unroll
+      for (int blk = 0; blk < D / 64; ++blk) {
+        umma::tile_load(umma::s32(sX) + blk * 16384, &mx1.map, blk * 64, s0, hs * mx1.head, b * mx1.batch, &x_full);
+        umma::tile_load(umma::s32(sX) + XB + blk * 16384, &mx2.map, blk * 64, s0, hs * mx2.head, b * mx2.batch, &x_full);
+      }
+    }
+    int raw = 0, n = 0;
+    for (; n < total; ++n) {
+      const int s = n % NS, m0 = (range.x + n % nt) * 64, hq = first_head + n / nt, hy = KEYS ? hq : hs / a.group;
+      if (n >= NS) ok = warp_wait(&y_free[s], (uint32_t)(n / NS - 1) & 1);
+      if (!ok) break;
+      // moving rows that no pair uses may hold an infinity (see the forward kernel)
+      bool clear = !KEYS && m0 + 64 > m.len && m.len < a.nk;
+      if (a.rq) clear |= (KEYS ? a.rq[(long long)b * a.tq + m0 / 64] : a.rk[(long long)b * a.tk + m0 / 64]).z != 0;
+      unsigned long long* bar = clear ? &y_raw : &y_full[s];
+      char* y = sY + s * 2 * YB;
+      if (one) {
+        umma::mbar_expect_tx(bar, 2 * YB);
+#pragma unroll
+        for (int blk = 0; blk < D / 64; ++blk) {
+          umma::tile_load(umma::s32(y) + blk * 8192, &my1.map, blk * 64, m0, hy * my1.head, b * my1.batch, bar);
+          umma::tile_load(umma::s32(y) + YB + blk * 8192, &my2.map, blk * 64, m0, hy * my2.head, b * my2.batch, bar);
+        }
+      }
+      if (KEYS) {
+        const long long at = ((long long)b * a.Hq + hq) * a.nq + m0;
+#pragma unroll
+        for (int u = 0; u < 64; u += 32) {
+          const bool in = m0 + u + lane < a.nq;
+          sL[s][u + lane] = in ? a.lse[at + u + lane] * kLog2e : 0.f;
+          sD[s][u + lane] = in ? a.delta[at + u + lane] : 0.f;
+        }
+        __syncwarp();
+        if (one) umma::mbar_arrive(&l_full[s]);
+      }
+      if (clear) {
+        ok = warp_wait(&y_raw, raw++ & 1);
+        auto keep = [&](int r) {
+          const int row = m0 + r;
+          return KEYS ? row >= a.nq || dq[row] >= 0 : row >= a.nk || (row < m.len && !(dk && dk[row] < 0));
+        };
+        tile_clear<D>(y, 64, keep);
+        if (KEYS) tile_clear<D>(y + YB, 64, keep);
+        if (one) umma::mbar_arrive(&y_full[s]);
+        if (!ok) { ++n; break; }
+      }
+    }
+    if (!ok)                                                                 // no copy is in flight when the CTA ends
+      for (int s = 0; s < NS; ++s)
+        if (n > s) umma::mbar_wait(&y_full[s], (uint32_t)((n - 1 - s) / NS) & 1);
+  } else if (warp == 9) {                                                    // products
+    if (umma::elect_one() && total > 0) {
+      const uint32_t id_s = umma::instr_desc(64, false, false), id_a = umma::instr_desc(D, false, true);
+      const int steps = a.d / 16;
+      const uint32_t x1 = umma::s32(sX), x2 = x1 + XB, y0 = umma::s32(sY);
+      auto scores = [&](int n) {                                             // S and dP of tile n
+        const int s = n % NS, buf = n & 1;
+        const uint32_t y1 = y0 + s * 2 * YB, y2 = y1 + YB;
+        ok = ok && umma::mbar_wait(&y_full[s], (uint32_t)(n / NS) & 1);
+        if (!ok) return;
+        umma::fence_after_sync();
+        for (int ks = 0; ks < steps; ++ks)
+          umma::mma(tm + buf * 128, umma::rows_desc(x1, 128, ks), umma::rows_desc(y1, 64, ks), id_s, ks > 0);
+        for (int ks = 0; ks < steps; ++ks)
+          umma::mma(tm + buf * 128 + 64, umma::rows_desc(x2, 128, ks), umma::rows_desc(y2, 64, ks), id_s, ks > 0);
+        umma::commit(&s_full[buf]);
+      };
+      ok = umma::mbar_wait(&x_full, 0);
+      umma::fence_after_sync();
+      scores(0);
+      if (total > 1) scores(1);
+      for (int n = 0; n < total && ok; ++n) {
+        const int s = n % NS, buf = n & 1;
+        const uint32_t y1 = y0 + s * 2 * YB, y2 = y1 + YB;
+        ok = umma::mbar_wait(&p_ready[buf], (uint32_t)(n >> 1) & 1);
+        if (!ok) break;
+        umma::fence_after_sync();
+        // a warp leaves its 32 columns in 16 packed ones at the place it read them from
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          const uint32_t at = tm + buf * 128 + (ks >> 1) * 32 + (ks & 1) * 8;
+          if (KEYS) umma::mma_ta(tm + ACC1, at, umma::cols_desc(y2, 64, ks), id_a, n > 0 || ks > 0);
+          umma::mma_ta(tm + ACC2, at + 64, umma::cols_desc(y1, 64, ks), id_a, n > 0 || ks > 0);
+        }
+        if (n + NS < total) umma::commit(&y_free[s]);                        // only where the copying warp waits for it
+        if (n + 2 < total) scores(n + 2);
+      }
+      if (ok) umma::commit(&acc_full);
+      else { umma::commit(&spare); umma::mbar_wait(&spare, 0); }             // no product is in flight when the CTA ends
+    }
+  } else {                                                                   // exponentials
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane, r = s0 + row;
+    const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
+    int doc, lo, hi;                                                         // moving tokens [lo, hi) are left by the masks but the documents'
+    float rowL = 0.f, rowD = 0.f;
+    if (KEYS) {
+      doc = dk && r < a.nk ? dk[r] : 0;
+      lo = m.first(r); hi = r < m.len && doc >= 0 ? a.nq : 0;
+    } else {
+      doc = dq && r < a.nq ? dq[r] : 0;
+      lo = 0; hi = r < a.nq && doc >= 0 ? m.limit(r) : 0;
+      // delta: two threads a row, half the channels each
+      const long long at = (long long)blockIdx.y * a.nq + r;
+      float v = 0.f;
+      if (r < a.nq) {
+        const bf16* o = static_cast<const bf16*>(a.o.p) + b * a.o.b + hs * a.o.h + r * a.o.t + half * (a.d / 2);
+        const bf16* g = static_cast<const bf16*>(a.dout.p) + b * a.dout.b + hs * a.dout.h + r * a.dout.t + half * (a.d / 2);
+        for (int c = 0; c < a.d / 2; c += 4) {
+          const float4 x = ld4(o + c), y = ld4(g + c);
+          v += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
+        }
+        rowL = a.lse[at] * kLog2e;
+      }
+      sDelta[half][row] = v;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      rowD = sDelta[0][row] + sDelta[1][row];
+      if (half == 0 && r < a.nq) a.delta[at] = rowD;
+    }
+    const int* dm = KEYS ? dq : dk;
+    const int nm = KEYS ? a.nq : a.nk;
+    for (int n = 0; n < total; ++n) {
+      const int buf = n & 1, s = n % NS, m0 = (range.x + n % nt) * 64, c0 = half * 32;
+      const SmScore sc = sm_score_of(a, first_head + n / nt);
+      const bool whole = KEYS ? s0 + 128 <= a.nk && sm_whole(a, m, b, m0, m0 + 64, s0, s0 + 128) : sm_whole(a, m, b, s0, s0 + 128, m0, m0 + 64);
+      const uint32_t ts = tm + quarter + buf * 128 + c0;
+      ok = (!KEYS || warp_wait(&l_full[s], (uint32_t)(n / NS) & 1)) && warp_wait(&s_full[buf], (uint32_t)(n >> 1) & 1);
+      if (!ok) break;
+      umma::fence_after_sync();
+      float x[32], g[32];
+      umma::tmem_ld32_async(ts, x);
+      umma::tmem_ld32_async(ts + 64, g);
+      umma::tmem_ld_wait();
+      umma::tie32(x);
+      umma::tie32(g);
+      uint32_t left = 0xffffffffu;                                           // columns that the masks leave
+      if (!whole) {
+        const int from = max(lo - m0 - c0, 0), to = min(max(hi - m0 - c0, 0), 32);
+        left = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & (from < 32 ? 0xffffffffu << from : 0u);
+        if (dm)
+#pragma unroll 4
+          for (int e = 0; e < 32; ++e) {
+            const int j = m0 + c0 + e, id = j < nm ? __ldg(dm + j) : -1;     // the same address for the whole warp
+            if (id != doc) left &= ~(1u << e);
+          }
+      }
+      const float away = (float)(KEYS ? m0 + c0 + m.off - r : r + m.off - m0 - c0);   // position of the query less the key's, column 0
+      uint32_t wp[16], wd[16];
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        float L[4], Dl[4];
+        if (KEYS) {
+          const float4 u = *reinterpret_cast<const float4*>(&sL[s][c0 + e]), v = *reinterpret_cast<const float4*>(&sD[s][c0 + e]);
+          L[0] = u.x; L[1] = u.y; L[2] = u.z; L[3] = u.w;
+          Dl[0] = v.x; Dl[1] = v.y; Dl[2] = v.z; Dl[3] = v.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = e + k;
+          const float lse = KEYS ? L[k] : rowL, delta = KEYS ? Dl[k] : rowD;
+          float bend = 1.f, y;
+          if (CAP) {
+            const float t = sm_cap_r(x[c], sc);
+            bend = 4.f * t * (1.f - t);
+            y = fmaf(-2.f * sc.cap2, t, sc.cap2 - lse);
+          } else {
+            y = fmaf(x[c], sc.mul, -lse);
+          }
+          if (BIAS) y = fmaf(-sc.slope2, fabsf(away + (KEYS ? (float)c : -(float)c)), y);
+          float p = ex2(y), d = p * (g[c] - delta);
+          if (CAP) d *= bend;
+          if (!whole && !((left >> c) & 1u)) p = d = 0.f;
+          x[c] = p; g[c] = d;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (KEYS) wp[e] = umma::pack_bf16(x[2 * e], x[2 * e + 1]);
+        wd[e] = umma::pack_bf16(g[2 * e], g[2 * e + 1]);
+      }
+      if (KEYS) umma::tmem_st16(ts, wp);
+      umma::tmem_st16(ts + 64, wd);
+      umma::tmem_st_wait();
+      umma::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) umma::mbar_arrive(&p_ready[buf]);
+    }
+    if (total > 0) {
+      ok = ok && warp_wait(&acc_full, 0);
+      umma::fence_after_sync();
+    }
+    if (ok) {
+      // rows of this warp, its half of the channels, through its part of the stationary tiles (no product reads them any more)
+      constexpr int HC = D / 2, PR = HC / 8;
+      const int rows = (KEYS ? a.nk : a.nq) - s0 - (warp & 3) * 32, pieces = min(max(a.d - half * HC, 0), HC) / 8;
+#pragma unroll
+      for (int out = 0; out < (KEYS ? 2 : 1); ++out) {
+        char* stage = sX + out * XB + (warp * 32 * HC) * 2;
+        const float mul = out ? 1.f : a.scale;
+#pragma unroll
+        for (int c = 0; c < HC; c += 32) {
+          float o[32];
+          if (total > 0) {
+            umma::tmem_ld32_async(tm + quarter + (out ? ACC1 : ACC2) + half * HC + c, o);
+            umma::tmem_ld_wait();
+            umma::tie32(o);
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = total > 0 ? umma::pack_bf16(o[8 * q + 2 * e] * mul, o[8 * q + 2 * e + 1] * mul) : 0u;
+            *reinterpret_cast<uint4*>(stage + (lane * PR + ((c / 8 + q) ^ (lane & (PR - 1)))) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        __syncwarp();
+        const SmView& v = out ? a.dv : (KEYS ? a.dk : a.dq);
+        bf16* G = static_cast<bf16*>(v.p) + b * v.b + hs * v.h + half * HC;
+        const long long first = s0 + (warp & 3) * 32;
+        for (int e = lane; e < 32 * pieces; e += 32) {
+          const int rr = e / pieces, p = e % pieces;
+          if (rr < rows)
+            *reinterpret_cast<uint4*>(G + (first + rr) * v.t + p * 8) = *reinterpret_cast<const uint4*>(stage + (rr * PR + (p ^ (rr & (PR - 1)))) * 16);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  umma::fence_before_sync();
+  __syncthreads();
+  if (warp == 9) umma::tmem_dealloc(tm, 512);
+  umma::report_timeout(ok, a.dev_status, KEYS ? b * a.Hq + first_head : (int)blockIdx.y);
+}
+
+}  // namespace ln

@@ -87,7 +87,7 @@ def test_softmax_views_and_workspace():
         assert call(ok, ok, FAKE, need - 1) == -3
         assert call(ok, ok, None, need) == -1 and call(ok, ok, NEAR, need) == -1
         assert call(_view(t=68), ok, FAKE, need) == -1 and call(_view(None), ok, FAKE, need) == -1
-        assert call(ok, _view(t=32), FAKE, need) == -1
+        assert call(ok, _view(t=32), FAKE, need) == -1 and call(_view(t=0), ok, FAKE, need) == -1
     assert L.softmax_attention_fwd(ctypes.byref(p), ok, ok, ok, ok, None, FAKE, 1 << 40, None, None) == -1
 
 
