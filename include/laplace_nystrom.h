@@ -302,8 +302,8 @@ int laplace_nystrom_saved_array(const ln_problem* p, const char* name, int64_t i
  * projection's [B, n, heads, d] output, or of a cache); `data` is 16-byte aligned.  The stride of an axis of length one is not
  * looked at.  An input's stride may be zero (a broadcast axis; not the token axis of the softmax entry points, LN_ERR_ARG); the rows of an
  * output must be distinct (LN_ERR_ARG).  Both views
- * of a call are on the device that is current.  Sizes are positive (LN_ERR_ARG); more than 2^30 tokens an axis or 2^31 - 64
- * rows of a call are LN_ERR_UNSUPPORTED.
+ * of a call are on the device that is current.  Sizes are positive (LN_ERR_ARG); more than 2^30 tokens an axis (2^22 - 64 queries, and keys of
+ * a backward pass, of softmax attention) or 2^31 - 64 rows of a call are LN_ERR_UNSUPPORTED.
  */
 typedef struct ln_view { void* data; int64_t batch, head, token; } ln_view;
 

@@ -6,7 +6,6 @@ loaded, or a tensor is not on a CUDA device, the call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -178,7 +177,7 @@ def lib():
         L.laplace_attention_block_workspace_bytes.argtypes = [pp, pb]
         L.laplace_attention_block_fwd.argtypes = [pp, pb, vp, vp, vp, vp, vp, vp, sz, vp, vp]
         L.laplace_attention_block_bwd.argtypes = [pp, pb, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
-        pr, pv, ps = ctypes.POINTER(_CRope), ctypes.POINTER(_CView), ctypes.POINTER(_CSoftmax)
+        pr, pv, ps = ctypes.POINTER(_CRope), vp, ctypes.POINTER(_CSoftmax)
         L.rope_fwd.argtypes = L.rope_bwd.argtypes = [pr, i32, i32, i32, i32, pv, pv, pv, pv, vp]
         L.qk_norm_rope_fwd.argtypes = [pr, i32, i32, i32, i32, f32, vp, vp, pv, pv, pv, pv, vp]
         L.qk_norm_rope_bwd_workspace_bytes.restype = sz
@@ -482,10 +481,6 @@ def launch_count() -> int:
 
 
 # ------------------------------------------------------------------------------------------ rotary positions, head norms
-class _CView(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
-
-
 class _CRope(ctypes.Structure):
     _fields_ = [("d", ctypes.c_int32), ("r", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("turns", ctypes.c_void_p), ("factor", ctypes.c_float), ("pos", ctypes.c_void_p),
@@ -499,38 +494,51 @@ class _CSoftmax(ctypes.Structure):
                 ("slopes", ctypes.c_void_p), ("doc_q", ctypes.c_void_p), ("doc_k", ctypes.c_void_p)]
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    """The tensors' device as the current one, and `stream` (or that device's current stream) as the stream of the call, its
-    allocations included."""
+def _launch(device, stream, call):
+    """call(raw stream) with the tensors' device as the current one and `stream` (or that device's current stream) as the
+    stream of the call, its allocations included."""
     if device.type != "cuda":
         raise ValueError("tensor must live on a CUDA device (there is no CPU path)")
+    if stream is None and torch.cuda.current_device() == device.index:
+        return call(torch.cuda.current_stream().cuda_stream)
     if stream is not None and stream.device != device:
         raise ValueError(f"stream of {stream.device} for tensors on {device}")
     with torch.cuda.device(device):
         if stream is None:
-            yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-        else:
-            with torch.cuda.stream(stream):
-                yield ctypes.c_void_p(stream.cuda_stream)
+            return call(torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
 
 
-def _heads(name, t, like, shape):
-    """Checks one [B, H, n, d] tensor and returns its view for the C ABI."""
-    if t.dim() != 4 or tuple(t.shape) != tuple(shape):
+def _heads(name, t, shape, dtype, device):
+    """Checks one [B, H, n, d] tensor; its pointer and strides, the fields of an ln_view."""
+    stride = t.stride()
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if t.stride(3) != 1:
+    if t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {dtype} on {device}")
+    if stride[3] != 1:
         raise ValueError(f"{name}: the channels of a row must be adjacent")
-    return _CView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return t.data_ptr(), stride[0], stride[1], stride[2]
+
+
+def _views(fields):
+    """ln_view structures one behind the other: the array that holds them, and the address of each (None for a missing tensor)."""
+    held = (ctypes.c_int64 * (4 * len(fields)))(*[x for f in fields for x in (f or (0, 0, 0, 0))])
+    at = ctypes.addressof(held)
+    return held, [None if f is None else at + 32 * i for i, f in enumerate(fields)]
+
+
+def _new(t, shape=None):
+    """An output: contiguous, whatever the strides of its model."""
+    return torch.empty(t.shape if shape is None else shape, dtype=t.dtype, device=t.device)
 
 
 def _vector(name, t, dtype, shape, device):
     """Checks an optional contiguous tensor of the call and returns its pointer."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected a contiguous {dtype} {tuple(shape)} on {device}")
     return t.data_ptr()
 
@@ -605,12 +613,6 @@ class Rope:
                       self.factor, None if pos is None else pos.data_ptr(), pb, pt, int(start))
 
 
-def _qk_outputs(Q, K, Qo, Ko):
-    """Outputs of the query / key preparation: contiguous unless given."""
-    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    return (new(Q) if Qo is None else Qo), (None if K is None else new(K) if Ko is None else Ko)
-
-
 def _qk_shapes(rope, Q, K):
     if Q.dim() != 4 or (K is not None and K.dim() != 4):
         raise ValueError("Q and K must be [B, H, n, d]")
@@ -623,13 +625,16 @@ def _qk_shapes(rope, Q, K):
 
 def _run_rope(entry, rope, Q, K, pos, start, Qo, Ko, stream):
     B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    with _on(Q.device, stream) as st:
-        Qo, Ko = _qk_outputs(Q, K, Qo, Ko)
-        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
-        cr = rope.c(Q, B, n, pos, start)
-        _check(getattr(lib(), entry)(ctypes.byref(cr), B, n, Hq, Hk, view("Q", Q, qs), view("K", K, ks), view("output of Q", Qo, qs),
-                                     view("output of K", Ko, ks), st), entry)
-    return Qo, Ko
+    dtype, device = Q.dtype, Q.device
+
+    def call(st):
+        yq = _new(Q) if Qo is None else Qo
+        yk = None if K is None else _new(K) if Ko is None else Ko
+        pair = lambda k: None if k is None else _heads("K", k, ks, dtype, device)
+        held, v = _views((_heads("Q", Q, qs, dtype, device), pair(K), _heads("output of Q", yq, qs, dtype, device), pair(yk)))
+        _check(getattr(lib(), entry)(ctypes.byref(rope.c(Q, B, n, pos, start)), B, n, Hq, Hk, *v, st), entry)
+        return yq, yk
+    return _launch(device, stream, call)
 
 
 def rope_fwd(rope: Rope, Q, K=None, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
@@ -647,33 +652,40 @@ def qk_norm_rope_fwd(rope: Rope, Q, K, gq=None, gk=None, eps: float = 1e-6, pos=
     """Qr = rope(gq * Q / rms(Q)), Kr = rope(gk * K / rms(K)), rms over the d channels of every head, in one pass.  gq, gk: fp32 [d]
     or None; K may be None; positions, strides and outputs as in rope_fwd."""
     B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    with _on(Q.device, stream) as st:
-        Qr, Kr = _qk_outputs(Q, K, Qr, Kr)
-        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
-        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), Q.device)
-        cr = rope.c(Q, B, n, pos, start)
-        _check(lib().qk_norm_rope_fwd(ctypes.byref(cr), B, n, Hq, Hk, float(eps), gain("gq", gq), gain("gk", gk), view("Q", Q, qs),
-                                      view("K", K, ks), view("Qr", Qr, qs), view("Kr", Kr, ks), st), "qk_norm_rope_fwd")
-    return Qr, Kr
+    dtype, device = Q.dtype, Q.device
+
+    def call(st):
+        yq = _new(Q) if Qr is None else Qr
+        yk = None if K is None else _new(K) if Kr is None else Kr
+        pair = lambda k: None if k is None else _heads("K", k, ks, dtype, device)
+        held, v = _views((_heads("Q", Q, qs, dtype, device), pair(K), _heads("Qr", yq, qs, dtype, device), pair(yk)))
+        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), device)
+        _check(lib().qk_norm_rope_fwd(ctypes.byref(rope.c(Q, B, n, pos, start)), B, n, Hq, Hk, eps, gain("gq", gq), gain("gk", gk), *v, st),
+               "qk_norm_rope_fwd")
+        return yq, yk
+    return _launch(device, stream, call)
 
 
 def qk_norm_rope_bwd(rope: Rope, Q, K, dQr, dKr, gq=None, gk=None, eps: float = 1e-6, pos=None, start: int = 0, dQ=None, dK=None, stream=None):
     """Adjoint of qk_norm_rope_fwd: dQ, dK, dgq, dgk (fp32 [d]; None where the gain, or K, is None).  Q and K are the inputs of the
     forward call."""
     B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    with _on(Q.device, stream) as st:
-        dQ, dK = _qk_outputs(Q, K, dQ, dK)
-        view = lambda name, t, s: None if t is None else ctypes.byref(_heads(name, t, Q, s))
-        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), Q.device)
+    dtype, device = Q.dtype, Q.device
+
+    def call(st):
+        xq = _new(Q) if dQ is None else dQ
+        xk = None if K is None else _new(K) if dK is None else dK
+        pair = lambda name, k: None if k is None else _heads(name, k, ks, dtype, device)
+        held, v = _views((_heads("Q", Q, qs, dtype, device), pair("K", K), _heads("dQr", dQr, qs, dtype, device), pair("dKr", dKr),
+                          _heads("dQ", xq, qs, dtype, device), pair("dK", xk)))
+        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), device)
+        dgq, dgk = None if gq is None else _new(gq), None if gk is None or K is None else _new(gk)
         cr = rope.c(Q, B, n, pos, start)
-        pq, pk = gain("gq", gq), gain("gk", gk)
-        dgq = None if gq is None else torch.empty_like(gq)
-        dgk = None if gk is None or K is None else torch.empty_like(gk)
-        ws = _bytes(lib().qk_norm_rope_bwd_workspace_bytes(ctypes.byref(cr), B, n, Hq, Hk), Q.device)
-        _check(lib().qk_norm_rope_bwd(ctypes.byref(cr), B, n, Hq, Hk, float(eps), pq, pk, view("Q", Q, qs), view("K", K, ks),
-                                      view("dQr", dQr, qs), view("dKr", dKr, ks), view("dQ", dQ, qs), view("dK", dK, ks),
-                                      _ptr(dgq), _ptr(dgk), _ptr(ws), ws.numel(), st), "qk_norm_rope_bwd")
-    return dQ, dK, dgq, dgk
+        ws = _bytes(lib().qk_norm_rope_bwd_workspace_bytes(ctypes.byref(cr), B, n, Hq, Hk), device)
+        _check(lib().qk_norm_rope_bwd(ctypes.byref(cr), B, n, Hq, Hk, eps, gain("gq", gq), gain("gk", gk), *v, _ptr(dgq), _ptr(dgk),
+                                      ws.data_ptr(), ws.numel(), st), "qk_norm_rope_bwd")
+        return xq, xk, dgq, dgk
+    return _launch(device, stream, call)
 
 
 # ------------------------------------------------------------------------------------------ softmax attention
@@ -716,38 +728,38 @@ def softmax_attention_fwd(sp: SoftmaxAttention, Q, K, V, O=None, lse=None, ws=No
     that the masks leave empty gets O = 0, lse = -inf.  Any strides with adjacent channels.  ``ws``: a uint8 tensor of
     softmax_attention_workspace_bytes(...), or None; calls that may overlap need one each."""
     cs = sp.c(Q, K)
-    qs, ks = tuple(Q.shape), (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    with _on(Q.device, stream) as st:
-        if O is None:
-            O = torch.empty(qs, dtype=Q.dtype, device=Q.device)
-        if lse is None:
-            lse = torch.empty(qs[:3], dtype=torch.float32, device=Q.device)
-        if ws is None:
-            ws = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 0), Q.device)
-        view = lambda name, t, s: ctypes.byref(_heads(name, t, Q, s))
-        _check(lib().softmax_attention_fwd(ctypes.byref(cs), view("Q", Q, qs), view("K", K, ks), view("V", V, ks), view("O", O, qs),
-                                           _vector("lse", lse, torch.float32, qs[:3], Q.device), _ptr(ws), ws.numel(),
-                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), Q.device), st),
-               "softmax_attention_fwd")
-    return O, lse
+    qs, ks = Q.shape, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
+    dtype, device = Q.dtype, Q.device
+
+    def call(st):
+        out = _new(Q) if O is None else O
+        sums = torch.empty(qs[:3], dtype=torch.float32, device=device) if lse is None else lse
+        work = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 0), device) if ws is None else ws
+        held, v = _views((_heads("Q", Q, qs, dtype, device), _heads("K", K, ks, dtype, device), _heads("V", V, ks, dtype, device),
+                          _heads("O", out, qs, dtype, device)))
+        _check(lib().softmax_attention_fwd(ctypes.byref(cs), *v, _vector("lse", sums, torch.float32, qs[:3], device), _ptr(work), work.numel(),
+                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), device), st), "softmax_attention_fwd")
+        return out, sums
+    return _launch(device, stream, call)
 
 
 def softmax_attention_bwd(sp: SoftmaxAttention, Q, K, V, O, lse, dO, dQ=None, dK=None, dV=None, ws=None, dev_status=None, stream=None):
     """Adjoint of softmax_attention_fwd: dQ, dK, dV.  O and lse are the forward call's."""
     cs = sp.c(Q, K)
-    qs, ks = tuple(Q.shape), (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    with _on(Q.device, stream) as st:
-        new = lambda s: torch.empty(s, dtype=Q.dtype, device=Q.device)
-        dQ, dK, dV = new(qs) if dQ is None else dQ, new(ks) if dK is None else dK, new(ks) if dV is None else dV
-        if ws is None:
-            ws = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 1), Q.device)
-        view = lambda name, t, s: ctypes.byref(_heads(name, t, Q, s))
-        _check(lib().softmax_attention_bwd(ctypes.byref(cs), view("Q", Q, qs), view("K", K, ks), view("V", V, ks), view("O", O, qs),
-                                           _vector("lse", lse, torch.float32, qs[:3], Q.device), view("dO", dO, qs), view("dQ", dQ, qs),
-                                           view("dK", dK, ks), view("dV", dV, ks), _ptr(ws), ws.numel(),
-                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), Q.device), st),
+    qs, ks = Q.shape, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
+    dtype, device = Q.dtype, Q.device
+
+    def call(st):
+        gq, gk, gv = _new(Q) if dQ is None else dQ, _new(Q, ks) if dK is None else dK, _new(Q, ks) if dV is None else dV
+        work = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 1), device) if ws is None else ws
+        one = lambda name, t, s: _heads(name, t, s, dtype, device)
+        held, v = _views((one("Q", Q, qs), one("K", K, ks), one("V", V, ks), one("O", O, qs), one("dO", dO, qs), one("dQ", gq, qs), one("dK", gk, ks),
+                          one("dV", gv, ks)))
+        _check(lib().softmax_attention_bwd(ctypes.byref(cs), *v[:4], _vector("lse", lse, torch.float32, qs[:3], device), *v[4:], _ptr(work),
+                                           work.numel(), _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), device), st),
                "softmax_attention_bwd")
-    return dQ, dK, dV
+        return gq, gk, gv
+    return _launch(device, stream, call)
 
 
 # ------------------------------------------------------------------------------------------ profiling aid

@@ -7,6 +7,7 @@
 #include "ln_host.cuh"
 #include "ln_rope.cuh"
 #include "ln_softmax_simt.cuh"
+#include "ln_softmax_step.cuh"
 #include "ln_softmax_bwd_umma.cuh"
 #include "ln_softmax_umma.cuh"
 
@@ -15,7 +16,7 @@ using namespace ln::host;
 
 namespace {
 
-constexpr long long kMostTokens = 1ll << 30, kMostRows = (1ll << 31) - 64;
+constexpr long long kMostTokens = 1ll << 30, kMostRows = (1ll << 31) - 64, kMostTiled = 65535ll * 64;
 
 // Strides of the three outer axes as the kernels use them (an axis of length one has none); false if the view cannot be read
 // in 16-byte pieces, or if it is an output whose rows overlap.
@@ -111,7 +112,7 @@ int run_qk(const ln_rope* p, int mode, float sign, int B, int n, int Hq, int Hk,
 }
 
 // ------------------------------------------------------------------------------------------ softmax attention
-int check_softmax(const ln_softmax* p) {
+int check_softmax(const ln_softmax* p, bool bwd) {
   if (!p || p->B <= 0 || p->Hq <= 0 || p->Hk <= 0 || p->nq <= 0 || p->nk <= 0 || p->d <= 0 || p->Hq % p->Hk) return LN_ERR_ARG;
   if (p->dtype != LN_F32 && p->dtype != LN_BF16) return LN_ERR_ARG;
   if (!(p->scale > 0.f) || !isfinite(p->scale) || !(p->cap >= 0.f) || !isfinite(p->cap) || (p->causal != 0 && p->causal != 1)) return LN_ERR_ARG;
@@ -119,15 +120,38 @@ int check_softmax(const ln_softmax* p) {
   const void* words[] = {p->prefix, p->kv_len, p->slopes, p->doc_q, p->doc_k};
   for (const void* w : words)
     if (reinterpret_cast<uintptr_t>(w) & 3u) return LN_ERR_ARG;
-  if ((p->d != 32 && p->d != 64 && p->d != 128) || (long long)p->B * p->Hq > 65535 || p->nq > kMostTokens || p->nk > kMostTokens) return LN_ERR_UNSUPPORTED;
+  if ((p->d != 32 && p->d != 64 && p->d != 128) || (long long)p->B * p->Hq > 65535 || p->nq > kMostTiled || p->nk > (bwd ? kMostTiled : kMostTokens)) return LN_ERR_UNSUPPORTED;
   return LN_OK;
 }
 
-// Workspace: the documents of every 64 tokens, and (backward) delta.
-struct SmWork { int4 *rq, *rk; float* delta; size_t bytes; };
+// A serving step: the rows that share a key head fit one 16-row tile.  Its keys are split over CTAs, four for every SM in all and
+// 256 keys at least.
+bool is_step(const ln_softmax* p) { return (long long)(p->Hq / p->Hk) * p->nq <= ST_ROWS; }
+StepPlan plan_step(const ln_softmax* p) {
+  const long long heads = (long long)p->B * p->Hk, want = (4ll * sm_count() + heads - 1) / heads;
+  long long chunk = (p->nk + want - 1) / want;
+  chunk = (chunk + 127) / 128 * 128;
+  if (chunk < 256) chunk = 256;
+  StepPlan s;
+  s.chunk = (int)chunk; s.splits = (int)cdiv(p->nk, chunk);
+  return s;
+}
+
+// Workspace: the documents of every 64 tokens, (backward) delta, (forward, a step) the splits' partial results.
+struct SmWork { int4 *rq, *rk; float* delta; StepPart part; size_t bytes; };
 SmWork carve_softmax(const ln_softmax* p, bool bwd, void* base) {
   Carver c(base);
   SmWork w = {};
+  if (!bwd && is_step(p)) {
+    const StepPlan s = plan_step(p);
+    const size_t rows = (size_t)p->B * p->Hq * p->nq * s.splits;
+    if (s.splits > 1) {
+      w.part.o = c.take(rows * p->d);
+      w.part.ml = reinterpret_cast<float2*>(c.take(rows * 2));
+    }
+    w.bytes = c.off;
+    return w;
+  }
   if (p->doc_q) {
     w.rq = reinterpret_cast<int4*>(c.take((size_t)p->B * cdiv(p->nq, 64) * 4));
     w.rk = reinterpret_cast<int4*>(c.take((size_t)p->B * cdiv(p->nk, 64) * 4));
@@ -157,15 +181,34 @@ void softmax_docs(const SmArgs& a, const SmWork& w, cudaStream_t st) {
   if (a.doc_q) LN_LAUNCH("k_sm_docs", st, enqueue(k_sm_docs, dim3(a.tq + a.tk, a.B), 32, 0, st, a.doc_q, a.doc_k, a.nq, a.nk, a.tq, a.tk, w.rq, w.rk));
 }
 
+void softmax_step(const ln_softmax* p, const SmArgs& a, const SmWork& w, cudaStream_t st) {
+  const StepPlan s = plan_step(p);
+  const dim3 grid(s.splits, a.B * a.Hk);
+  auto go = [&](auto kern) { LN_LAUNCH("k_softmax_step", st, enqueue(kern, grid, ST_WARPS * 32, 0, st, a, s, w.part)); };
+  auto f32 = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    const int rows = a.group * a.nq;
+    if (rows == 1) go(k_softmax_step_f32<D, 1>); else if (rows <= 4) go(k_softmax_step_f32<D, 4>); else go(k_softmax_step_f32<D, ST_ROWS>);
+  };
+  if (p->dtype == LN_BF16) { if (p->d == 32) go(k_softmax_step<32>); else if (p->d == 64) go(k_softmax_step<64>); else go(k_softmax_step<128>); }
+  else if (p->d == 32) f32(std::integral_constant<int, 32>());
+  else if (p->d == 64) f32(std::integral_constant<int, 64>());
+  else f32(std::integral_constant<int, 128>());
+  if (s.splits == 1) return;
+  const dim3 rows(cdiv((long long)a.B * a.Hq * a.nq, 4));
+  if (p->dtype == LN_BF16) LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<bf16>, rows, 128, 0, st, a, s, w.part));
+  else LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<float>, rows, 128, 0, st, a, s, w.part));
+}
+
 template <typename T, int D> void softmax_fwd_simt(const SmArgs& a, cudaStream_t st) {
   want_smem(k_softmax_fwd<T, D>, sm_fwd_smem<D>());
-  LN_LAUNCH("k_softmax_fwd", st, enqueue(k_softmax_fwd<T, D>, dim3(cdiv(a.nq, SS), a.B * a.Hq), 256, sm_fwd_smem<D>(), st, a));
+  LN_LAUNCH("k_softmax_fwd", st, enqueue(k_softmax_fwd<T, D>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_fwd_smem<D>(), st, a));
 }
 template <typename T, int D> void softmax_bwd_simt(const SmArgs& a, cudaStream_t st) {
   want_smem(k_softmax_bwd<T, D, false>, sm_bwd_smem<D, false>());
-  LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<T, D, false>, dim3(cdiv(a.nq, SS), a.B * a.Hq), 256, sm_bwd_smem<D, false>(), st, a));
+  LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<T, D, false>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_bwd_smem<D, false>(), st, a));
   want_smem(k_softmax_bwd<T, D, true>, sm_bwd_smem<D, true>());
-  LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<T, D, true>, dim3(cdiv(a.nk, SS), a.B * a.Hk), 256, sm_bwd_smem<D, true>(), st, a));
+  LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<T, D, true>, dim3(a.B * a.Hk, cdiv(a.nk, SS)), 256, sm_bwd_smem<D, true>(), st, a));
 }
 
 // The driver's encoder of tensor maps, by name (the library is not linked against the driver).
@@ -198,7 +241,7 @@ template <int D> int softmax_fwd_umma(const SmArgs& a, cudaStream_t st) {
   if (!tile_map(a.q, a.B, a.Hq, a.nq, a.d, 128, &q) || !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 128, &k) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 128, &v)) return LN_ERR_CUDA;
   auto go = [&](auto kern) {
     want_smem(kern, SuFwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(cdiv(a.nq, 256), a.B * a.Hq), SU_THREADS, SuFwd<D>::kSmem, st, a, q, k, v));
+    LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(a.B * a.Hq, cdiv(a.nq, 256)), SU_THREADS, SuFwd<D>::kSmem, st, a, q, k, v));
   };
   if (a.cap > 0.f) { if (a.slopes) go(k_softmax_fwd_umma<D, true, true>); else go(k_softmax_fwd_umma<D, true, false>); }
   else { if (a.slopes) go(k_softmax_fwd_umma<D, false, true>); else go(k_softmax_fwd_umma<D, false, false>); }
@@ -212,9 +255,9 @@ template <int D> int softmax_bwd_umma(const SmArgs& a, cudaStream_t st) {
       !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 64, &mk) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 64, &mv)) return LN_ERR_CUDA;
   auto go = [&](auto q, auto kv) {
     want_smem(q, SuBwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_bwd_q", st, enqueue(q, dim3(cdiv(a.nq, 128), a.B * a.Hq), SU_THREADS, SuBwd<D>::kSmem, st, a, sq, sdo, mk, mv));
+    LN_LAUNCH("k_softmax_bwd_q", st, enqueue(q, dim3(a.B * a.Hq, cdiv(a.nq, 128)), SU_THREADS, SuBwd<D>::kSmem, st, a, sq, sdo, mk, mv));
     want_smem(kv, SuBwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(cdiv(a.nk, 128), a.B * a.Hk), SU_THREADS, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
+    LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(a.B * a.Hk, cdiv(a.nk, 128)), SU_THREADS, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
   };
   if (a.cap > 0.f) {
     if (a.slopes) go(k_softmax_bwd_umma<D, true, true, false>, k_softmax_bwd_umma<D, true, true, true>);
@@ -271,14 +314,14 @@ int qk_norm_rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t
 }
 
 size_t softmax_attention_workspace_bytes(const ln_softmax* p, int32_t backward) {
-  if (check_softmax(p) != LN_OK) return 0;
+  if (check_softmax(p, backward != 0) != LN_OK) return 0;
   const size_t n = carve_softmax(p, backward != 0, nullptr).bytes;
   return n ? n : 256;                               // never 0 for a valid problem
 }
 
 int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, float* lse, void* ws,
                           size_t ws_bytes, int32_t* dev_status, void* stream) {
-  const int rc = check_softmax(p);
+  const int rc = check_softmax(p, false);
   if (rc != LN_OK) return rc;
   const SmWork w = carve_softmax(p, false, ws);
   SmArgs a = softmax_args(p, w, dev_status);
@@ -288,6 +331,7 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   a.lse = lse;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dev_status) cudaMemsetAsync(dev_status, 0, sizeof(int32_t) * (size_t)p->B * p->Hq, st);
+  if (is_step(p)) { softmax_step(p, a, w, st); return launch_ok(); }
   softmax_docs(a, w, st);
   int made = LN_OK;
   if (p->dtype == LN_BF16) made = p->d == 128 ? softmax_fwd_umma<128>(a, st) : softmax_fwd_umma<64>(a, st);
@@ -301,7 +345,7 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
 int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* K, const ln_view* V, const ln_view* O, const float* lse,
                           const ln_view* dO, const ln_view* dQ, const ln_view* dK, const ln_view* dV, void* ws, size_t ws_bytes, int32_t* dev_status,
                           void* stream) {
-  const int rc = check_softmax(p);
+  const int rc = check_softmax(p, true);
   if (rc != LN_OK) return rc;
   const SmWork w = carve_softmax(p, true, ws);
   SmArgs a = softmax_args(p, w, dev_status);

@@ -36,8 +36,8 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   __shared__ float sDelta[KEYS ? 1 : 2][128];
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.y / H, hs = blockIdx.y % H;
-  const int s0 = (KEYS ? (int)blockIdx.x : (int)gridDim.x - 1 - (int)blockIdx.x) * 128;     // the longest causal rows first
+  const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.x / H, hs = blockIdx.x % H;
+  const int s0 = (KEYS ? (int)blockIdx.y : (int)gridDim.y - 1 - (int)blockIdx.y) * 128;     // the longest causal rows first
   const SmMask m(a, b);
   const int2 range = sm_range<128, KEYS>(a, m, b, s0, sh);
   const int nt = range.y - range.x, total = KEYS ? nt * a.group : nt;
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
       doc = dq && r < a.nq ? dq[r] : 0;
       lo = 0; hi = r < a.nq && doc >= 0 ? m.limit(r) : 0;
       // delta: two threads a row, half the channels each
-      const long long at = (long long)blockIdx.y * a.nq + r;
+      const long long at = (long long)blockIdx.x * a.nq + r;
       float v = 0.f;
       if (r < a.nq) {
         const bf16* o = static_cast<const bf16*>(a.o.p) + b * a.o.b + hs * a.o.h + r * a.o.t + half * (a.d / 2);
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   umma::fence_before_sync();
   __syncthreads();
   if (warp == 9) umma::tmem_dealloc(tm, 512);
-  umma::report_timeout(ok, a.dev_status, KEYS ? b * a.Hq + first_head : (int)blockIdx.y);
+  umma::report_timeout(ok, a.dev_status, KEYS ? b * a.Hq + first_head : (int)blockIdx.x);
 }
 
 }  // namespace ln

@@ -85,8 +85,8 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
   extern __shared__ __align__(16) float sm_smem[];
   float *Qs = sm_smem, *Ks = Qs + SS * (D + 4), *Vs = Ks + SS * (D + 4), *Ps = Vs + SS * (D + 4);
   __shared__ int sh[2];
-  const int b = blockIdx.y / a.Hq, h = blockIdx.y % a.Hq, hk = h / a.group;
-  const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * SS, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;   // long causal rows first
+  const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, hk = h / a.group;
+  const int i0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * SS, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;   // long causal rows first
   const T* Q = static_cast<const T*>(a.q.p) + b * a.q.b + h * a.q.h;
   const T* K = static_cast<const T*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const T* V = static_cast<const T*>(a.v.p) + b * a.v.b + hk * a.v.h;
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
     const float inv = sum[k] > 0.f ? 1.f / sum[k] : (sum[k] == 0.f ? 0.f : sum[k]);     // NaN stays
 #pragma unroll
     for (int q = 0; q < D / 16; ++q) O[i * a.o.t + ColMap<D>::col(tx, q)] = from_f<T>(acc[k][q] * inv);
-    if (tx == 0) a.lse[(long long)blockIdx.y * a.nq + i] = sum[k] == 0.f ? -INFINITY : mx[k] * kLn2 + logf(sum[k]);
+    if (tx == 0) a.lse[(long long)blockIdx.x * a.nq + i] = sum[k] == 0.f ? -INFINITY : mx[k] * kLn2 + logf(sum[k]);
   }
 }
 
@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmA
   constexpr int TF = SS * (D + 4);
   float *X1 = sm_smem, *X2 = X1 + TF, *Y1 = X2 + TF, *Y2 = Y1 + TF, *S = Y2 + TF, *P = S + SS * SSG, *L = S + (KEYS ? 2 : 1) * SS * SSG, *Dl = L + SS;
   __shared__ int sh[2];
-  const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.y / H, hs = blockIdx.y % H;
-  const int tile = KEYS ? blockIdx.x : gridDim.x - 1 - blockIdx.x, s0 = tile * SS;      // long causal rows first
+  const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.x / H, hs = blockIdx.x % H;
+  const int tile = KEYS ? blockIdx.y : gridDim.y - 1 - blockIdx.y, s0 = tile * SS;      // long causal rows first
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const SmMask m(a, b);
   const int* dq = a.doc_q ? a.doc_q + (long long)b * a.nq : nullptr;
@@ -198,8 +198,8 @@ __global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmA
     v += __shfl_xor_sync(0xffffffffu, v, 2);
     if ((tid & 3) == 0) {
       Dl[r] = v;
-      L[r] = i < a.nq ? a.lse[(long long)blockIdx.y * a.nq + i] * kLog2e : 0.f;
-      if (i < a.nq) a.delta[(long long)blockIdx.y * a.nq + i] = v;
+      L[r] = i < a.nq ? a.lse[(long long)blockIdx.x * a.nq + i] * kLog2e : 0.f;
+      if (i < a.nq) a.delta[(long long)blockIdx.x * a.nq + i] = v;
     }
   }
   float a1[4][D / 16], a2[4][D / 16];

@@ -1,0 +1,368 @@
+// Softmax attention of a few queries (a serving step): the rows of a key head are its group's query heads times nq <= 16 queries,
+// and a long cache is read once for all of them.
+//
+// Bound by memory traffic: the keys and values of a head, once.  The keys are split over CTAs, over the eight warps of a CTA in
+// turns of 16 keys, and every warp keeps maximum, sum and accumulator of its own; warps are joined through shared memory, CTAs
+// by k_softmax_join.  bf16 rows go straight from global memory into the operands of mma.sync (m16n8k16, fp32 accumulate; 16 rows
+// are all a serving step has, a tcgen05 tile would be 128): both products sum over an axis whose order is free, so a lane's
+// 16-byte piece of a row IS its share of an operand, and neither K nor V passes through shared memory.
+//   S = Q K^T   B = K^T: lane (g, c) = (lane / 4, lane % 4) holds channels 32 l + 8 c .. of key g, which stand for k-steps 2 l, 2 l + 1
+//   O = A V     B = V:   lane (g, c) holds channels g d / 8 .. of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9; column tile j is channel g d / 8 + j
+#pragma once
+#include "ln_mma.cuh"
+#include "ln_softmax.cuh"
+
+namespace ln {
+
+constexpr int ST_ROWS = 16, ST_WARPS = 8;
+
+struct StepPlan { int chunk, splits; };              // keys a CTA, CTAs a key head
+struct StepPart { float* o; float2* ml; };           // [row][split][d] partial outputs, maximum (base 2) and sum of every partial
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { uint32_t r; asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel)); return r; }
+
+// Score in base 2 from the product, with the cap through the accurate tanh: a step has few scores.
+__device__ __forceinline__ float step_score(float dot, const SmArgs& a, float slope2, int dist) {
+  float x = dot * a.scale;
+  if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
+  return fmaf(x, kLog2e, -slope2 * (float)abs(dist));
+}
+
+// Pieces of 16 (d = 64, 128) or 8 bytes (d = 32) of a row, streamed past L1.
+template <int N> __device__ __forceinline__ void step_load(const bf16* p, bool in, uint32_t (&r)[N]) {
+  if (N == 2) {
+    uint2 v = make_uint2(0u, 0u);
+    if (in) v = __ldg(reinterpret_cast<const uint2*>(p));
+    r[0] = v.x; r[1] = v.y;
+  } else {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (in) v = __ldg(reinterpret_cast<const uint4*>(p) + q);
+      r[4 * q] = v.x; r[4 * q + 1] = v.y; r[4 * q + 2] = v.z; r[4 * q + 3] = v.w;
+    }
+  }
+}
+
+// A CTA's joined accumulators: the result itself if it is the only split, else its part.  s_m, s_l [warp][pitch_r], s_o [row][pitch_o].
+template <typename T, int D>
+__device__ __forceinline__ void step_write(const SmArgs& a, const StepPlan& pl, const StepPart& part, int b, int hk, int split, int rows, const float* s_m,
+                                           const float* s_l, int pitch_r, const float* s_o, int pitch_o) {
+  for (int e = threadIdx.x; e < rows * D; e += ST_WARPS * 32) {
+    const int r = e / D, ch = e % D, h = hk * a.group + r / a.nq, i = r % a.nq;
+    const long long row = ((long long)b * a.Hq + h) * a.nq + i;
+    float t = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < ST_WARPS; ++w) t = fmaxf(t, s_m[w * pitch_r + r]);
+#pragma unroll
+    for (int w = 0; w < ST_WARPS; ++w) {
+      const float mw = s_m[w * pitch_r + r], lw = s_l[w * pitch_r + r];
+      l += mw == -INFINITY ? lw : lw * ex2(mw - t);                          // a sum of nothing is zero, NaN stays
+    }
+    const float o = s_o[r * pitch_o + ch];
+    if (pl.splits == 1) {
+      static_cast<T*>(a.o.p)[b * a.o.b + h * a.o.h + i * a.o.t + ch] = from_f<T>(l == 0.f ? 0.f : o / l);
+      if (ch == 0) a.lse[row] = l == 0.f ? -INFINITY : t * kLn2 + logf(l);
+    } else {
+      part.o[(row * pl.splits + split) * D + ch] = o;
+      if (ch == 0) part.ml[row * pl.splits + split] = make_float2(t, l);
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(ST_WARPS * 32) k_softmax_step(const __grid_constant__ SmArgs a, StepPlan pl, StepPart part) {
+  pdl_wait();
+  constexpr int KL = D / 32, VW = D / 16, NT = D / 8;      // 16-byte pieces of a key row a lane, words of a value row a lane, column tiles
+  const int split = blockIdx.x, hk = blockIdx.y % a.Hk, b = blockIdx.y / a.Hk;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  const SmMask m(a, b);
+  const int rows = a.group * a.nq;
+  const int k0 = split * pl.chunk, k1 = min(min(k0 + pl.chunk, m.len), m.limit(a.nq - 1));
+  const bf16* K = static_cast<const bf16*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const bf16* V = static_cast<const bf16*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
+  // rows g and g + 8 of this lane: query head, query, limit, document, slope
+  int lim[2], doc[2], pos[2];
+  float slope2[2];
+  uint32_t qa[2][KL * 4];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int r = g + 8 * s, hq = hk * a.group + r / a.nq, i = r % a.nq;
+    const bool in = r < rows;
+    doc[s] = in && a.doc_q ? a.doc_q[(long long)b * a.nq + i] : 0;
+    lim[s] = in && doc[s] >= 0 ? m.limit(i) : 0;
+    pos[s] = i + m.off;
+    slope2[s] = in && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
+#pragma unroll
+    for (int l = 0; l < KL; ++l) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (in) v = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.q.p) + b * a.q.b + hq * a.q.h + i * a.q.t + l * 32 + c * 8);
+      qa[s][4 * l] = v.x; qa[s][4 * l + 1] = v.y; qa[s][4 * l + 2] = v.z; qa[s][4 * l + 3] = v.w;
+    }
+  }
+  float acc[NT][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+
+  uint32_t kb[2][KL][4];
+  auto keys = [&](int j0) {                                // the 16 keys from j0: lane group g has keys j0 + g and j0 + 8 + g
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int j = j0 + 8 * t + g;
+#pragma unroll
+      for (int l = 0; l < KL; ++l) step_load(K + (long long)j * a.k.t + l * 32 + c * 8, j < k1, kb[t][l]);
+    }
+  };
+  int j0 = k0 + warp * 16;
+  if (j0 < k1) keys(j0);
+  for (; j0 < k1; j0 += ST_WARPS * 16) {
+    uint32_t vb[4][VW];                                    // keys j0 + 2 c, + 1, + 8, + 9: absent ones are zeros whatever they hold
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + 2 * c + (u & 1) + 8 * (u >> 1);
+      step_load(V + (long long)j * a.v.t + g * (D / 8), j < k1 && !(dk && dk[j] < 0), vb[u]);
+    }
+    float s[2][4] = {};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int l = 0; l < KL; ++l)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const uint32_t A[4] = {qa[0][4 * l + 2 * f], qa[1][4 * l + 2 * f], qa[0][4 * l + 2 * f + 1], qa[1][4 * l + 2 * f + 1]};
+          mma_bf16(s[t], A, kb[t][l][2 * f], kb[t][l][2 * f + 1]);
+        }
+    if (j0 + ST_WARPS * 16 < k1) keys(j0 + ST_WARPS * 16);
+    float ref[2], old[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int j = j0 + 8 * t + 2 * c + e;
+          const float x = step_score(s[t][2 * r + e], a, slope2[r], pos[r] - j);
+          s[t][2 * r + e] = j < lim[r] && j < k1 && (!dk || dk[j] == doc[r]) ? x : -INFINITY;
+          top = fmaxf(top, s[t][2 * r + e]);
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float now = fmaxf(mx[r], top);
+      ref[r] = now == -INFINITY ? 0.f : now;
+      old[r] = ex2(mx[r] - ref[r]);
+      mx[r] = now;
+      sum[r] *= old[r];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p = ex2(s[t][2 * r + e] - ref[r]);
+          s[t][2 * r + e] = p;
+          sum[r] += p;
+        }
+    }
+    const __nv_bfloat162 p0 = __floats2bfloat162_rn(s[0][0], s[0][1]), p1 = __floats2bfloat162_rn(s[0][2], s[0][3]);
+    const __nv_bfloat162 p2 = __floats2bfloat162_rn(s[1][0], s[1][1]), p3 = __floats2bfloat162_rn(s[1][2], s[1][3]);
+    const uint32_t A[4] = {*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1), *reinterpret_cast<const uint32_t*>(&p2),
+                           *reinterpret_cast<const uint32_t*>(&p3)};
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      acc[j][0] *= old[0]; acc[j][1] *= old[0]; acc[j][2] *= old[1]; acc[j][3] *= old[1];
+      const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+      mma_bf16(acc[j], A, prmt(vb[0][j >> 1], vb[1][j >> 1], sel), prmt(vb[2][j >> 1], vb[3][j >> 1], sel));
+    }
+  }
+  // join the warps: maxima and sums, then the accumulators in the warps' order, 16 x D floats at a time
+  __shared__ float s_m[ST_WARPS][ST_ROWS], s_l[ST_WARPS][ST_ROWS];
+  __shared__ float s_o[ST_ROWS][D + 4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 1);
+    sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 2);
+    if (c == 0) { s_m[warp][g + 8 * r] = mx[r]; s_l[warp][g + 8 * r] = sum[r]; }
+  }
+  __syncthreads();
+  float top[2] = {-INFINITY, -INFINITY}, f[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int w = 0; w < ST_WARPS; ++w) top[r] = fmaxf(top[r], s_m[w][g + 8 * r]);
+    f[r] = mx[r] == -INFINITY ? 0.f : ex2(mx[r] - top[r]);
+  }
+  for (int w = 0; w < ST_WARPS; ++w) {
+    if (w == warp)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {                     // column 2 c + (e & 1) of tile j: channel (2 c + (e & 1)) D / 8 + j
+          float* o = &s_o[g + 8 * (e >> 1)][(2 * c + (e & 1)) * (D / 8) + j];
+          const float v = acc[j][e] * f[e >> 1];
+          *o = w ? *o + v : v;
+        }
+    __syncthreads();
+  }
+  step_write<bf16, D>(a, pl, part, b, hk, split, rows, &s_m[0][0], &s_l[0][0], ST_ROWS, &s_o[0][0], D + 4);
+}
+
+// The same for fp32 storage on the CUDA cores (products with 24-bit operands), for up to RB rows.  A warp takes 32 keys a turn: lane
+// (g, c) has channels 16 l + 4 c .. of key g of a group of eight, four groups one after the other; a dot product is the four lanes'
+// shares added.  The exponentials go through shared memory, and every lane owns D / 32 channels of the accumulators.
+template <int D, int RB>
+__global__ void __launch_bounds__(ST_WARPS * 32) k_softmax_step_f32(const __grid_constant__ SmArgs a, StepPlan pl, StepPart part) {
+  pdl_wait();
+  constexpr int KL = D / 16, CD = D / 32;
+  const int split = blockIdx.x, hk = blockIdx.y % a.Hk, b = blockIdx.y / a.Hk;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  const SmMask m(a, b);
+  const int rows = a.group * a.nq;
+  const int k0 = split * pl.chunk, k1 = min(min(k0 + pl.chunk, m.len), m.limit(a.nq - 1));
+  const float* K = static_cast<const float*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const float* V = static_cast<const float*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
+  __shared__ __align__(16) float s_q[RB][D], s_p[ST_WARPS][32][RB], s_o[RB][D];
+  __shared__ int s_lim[RB], s_doc[RB], s_pos[RB];
+  __shared__ float s_slope[RB], s_m[ST_WARPS][RB], s_l[ST_WARPS][RB];
+  for (int e = tid; e < RB * D; e += ST_WARPS * 32) {
+    const int r = e / D, ch = e % D;
+    s_q[r][ch] = r < rows ? static_cast<const float*>(a.q.p)[b * a.q.b + (hk * a.group + r / a.nq) * a.q.h + (r % a.nq) * a.q.t + ch] : 0.f;
+  }
+  if (tid < RB) {
+    const int i = tid % a.nq, doc = tid < rows && a.doc_q ? a.doc_q[(long long)b * a.nq + i] : 0;
+    s_doc[tid] = doc;
+    s_lim[tid] = tid < rows && doc >= 0 ? m.limit(i) : 0;
+    s_pos[tid] = i + m.off;
+    s_slope[tid] = tid < rows && a.slopes ? a.slopes[hk * a.group + tid / a.nq] * kLog2e : 0.f;
+  }
+  __syncthreads();
+  float acc[RB][CD], mx[RB], sum[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    mx[r] = -INFINITY; sum[r] = 0.f;
+#pragma unroll
+    for (int q = 0; q < CD; ++q) acc[r][q] = 0.f;
+  }
+  for (int j0 = k0 + warp * 32; j0 < k1; j0 += ST_WARPS * 32) {
+    float s[RB][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int j = j0 + 8 * t + g;
+      float4 k[KL];
+#pragma unroll
+      for (int l = 0; l < KL; ++l) {
+        k[l] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j < k1) k[l] = __ldg(reinterpret_cast<const float4*>(K + (long long)j * a.k.t + l * 16 + c * 4));
+      }
+      const int doc = dk && j < k1 ? dk[j] : 0;
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        float d = 0.f;
+#pragma unroll
+        for (int l = 0; l < KL; ++l) {
+          const float4 q = *reinterpret_cast<const float4*>(&s_q[r][l * 16 + c * 4]);
+          d = fmaf(q.x, k[l].x, d); d = fmaf(q.y, k[l].y, d); d = fmaf(q.z, k[l].z, d); d = fmaf(q.w, k[l].w, d);
+        }
+        d += __shfl_xor_sync(0xffffffffu, d, 1);
+        d += __shfl_xor_sync(0xffffffffu, d, 2);
+        const float x = step_score(d, a, s_slope[r], s_pos[r] - j);
+        s[r][t] = j < k1 && j < s_lim[r] && (!dk || doc == s_doc[r]) ? x : -INFINITY;
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      float top = fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3]));
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float now = fmaxf(mx[r], top), ref = now == -INFINITY ? 0.f : now, old = ex2(mx[r] - ref);
+      mx[r] = now;
+      sum[r] *= old;
+#pragma unroll
+      for (int q = 0; q < CD; ++q) acc[r][q] *= old;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float p = ex2(s[r][t] - ref);
+        sum[r] += p;
+        if (c == (r & 3)) s_p[warp][8 * t + g][r] = p;
+      }
+    }
+    __syncwarp();
+    const int n = min(32, k1 - j0);
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      float v[CD];
+      const bool in = !(dk && dk[j0 + j] < 0);             // absent keys are zeros whatever they hold
+#pragma unroll
+      for (int q = 0; q < CD; ++q) v[q] = in ? __ldg(V + (long long)(j0 + j) * a.v.t + q * 32 + lane) : 0.f;
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const float p = s_p[warp][j][r];
+#pragma unroll
+        for (int q = 0; q < CD; ++q) acc[r][q] = fmaf(p, v[q], acc[r][q]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], o);
+    if (lane == 0) { s_m[warp][r] = mx[r]; s_l[warp][r] = sum[r]; }
+  }
+  __syncthreads();
+  for (int w = 0; w < ST_WARPS; ++w) {
+    if (w == warp)
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        float t = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < ST_WARPS; ++k) t = fmaxf(t, s_m[k][r]);
+        const float f = mx[r] == -INFINITY ? 0.f : ex2(mx[r] - t);
+#pragma unroll
+        for (int q = 0; q < CD; ++q) s_o[r][q * 32 + lane] = (w ? s_o[r][q * 32 + lane] : 0.f) + acc[r][q] * f;
+      }
+    __syncthreads();
+  }
+  step_write<float, D>(a, pl, part, b, hk, split, rows, &s_m[0][0], &s_l[0][0], RB, &s_o[0][0], D);
+}
+
+// Partial results of a row -> its output and lse.  One warp per row, the splits in order.
+template <typename T>
+__global__ void __launch_bounds__(128) k_softmax_join(const __grid_constant__ SmArgs a, StepPlan pl, StepPart part) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= (long long)a.B * a.Hq * a.nq) return;
+  const float2* ml = part.ml + row * pl.splits;
+  float top = -INFINITY;
+  for (int s = lane; s < pl.splits; s += 32) top = fmaxf(top, ml[s].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < pl.splits; s0 += 32) {
+    const float2 mine = s0 + lane < pl.splits ? ml[s0 + lane] : make_float2(-INFINITY, 0.f);
+    const float w = mine.x == -INFINITY ? 0.f : ex2(mine.x - top);
+    float part_l = mine.x == -INFINITY ? mine.y : mine.y * w;                  // NaN stays
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part_l += __shfl_xor_sync(0xffffffffu, part_l, o);
+    l += part_l;
+    const int n = min(32, pl.splits - s0);
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+      const float ws = __shfl_sync(0xffffffffu, w, s);
+      const float* o = part.o + (row * pl.splits + s0 + s) * a.d;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q * 32 < a.d) acc[q] = fmaf(ws, o[q * 32 + lane], acc[q]);
+    }
+  }
+  const int i = (int)(row % a.nq), h = (int)(row / a.nq % a.Hq), b = (int)(row / a.nq / a.Hq);
+  T* O = static_cast<T*>(a.o.p) + b * a.o.b + h * a.o.h + i * a.o.t;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q * 32 < a.d) O[q * 32 + lane] = from_f<T>(acc[q] * inv);
+  if (lane == 0) a.lse[row] = l == 0.f ? -INFINITY : top * kLn2 + logf(l);
+}
+
+}  // namespace ln

@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
   __shared__ uint32_t tmem_slot;
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const int bh = blockIdx.y, b = bh / a.Hq, h = bh % a.Hq, hk = h / a.group;
-  const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 256;                 // long causal rows first
+  const int bh = blockIdx.x, b = bh / a.Hq, h = bh % a.Hq, hk = h / a.group;
+  const int i0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * 256;                 // long causal rows first
   const SmMask m(a, b);
   const int2 range = sm_range<256, false>(a, m, b, i0, sh);
   const int nt = (range.y - range.x + 1) / 2, k0 = range.x * 64;             // key tiles of 128 from k0

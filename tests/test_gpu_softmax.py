@@ -136,6 +136,20 @@ def test_shared_heads(dtype, Hq, Hk, nq):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("Hq,Hk,nq", [(1, 1, 1), (4, 1, 1), (8, 4, 2), (16, 1, 1), (2, 2, 16), (3, 1, 5), (6, 2, 6)])
+def test_steps_over_a_long_cache(dtype, d, Hq, Hk, nq):
+    """Few queries, keys split over many CTAs: with up to 16 rows a key head the step kernels, with 18 the others."""
+    nk = 5003
+    Q, K, V, _ = _inputs(3, Hq, Hk, nq, nk, d, dtype, sigma=3.0)
+    kv = torch.tensor([nk, 517, 4999], dtype=torch.int32)
+    _compare(Q, K, V)
+    _compare(Q, K, V, causal=True, kv_len=kv, cap=15.0, slopes=_slopes(Hq), prefix=torch.tensor([0, 516, 5003], dtype=torch.int32))
+    dk = _docs(3, nk, 1)
+    _compare(Q, K, V, doc_q=dk[:, 2000:2000 + nq].contiguous(), doc_k=dk, kv_len=kv)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
 def test_long_row_and_large_scores(dtype):
     # scores of +-100 and more: the running maximum moves, the exponentials span the whole range
     Q, K, V, dO = _inputs(1, 2, 2, 130, 2100, 64, dtype, sigma=30.0)

@@ -14,8 +14,12 @@ FAKE = ctypes.c_void_p(4096)                       # never dereferenced: validat
 NEAR = ctypes.c_void_p(4100)                       # not on 16 bytes
 
 
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
 def _view(data=FAKE, b=4096, h=512, t=64):
-    return ctypes.byref(binding._CView(data.value if data else None, b, h, t))
+    return ctypes.byref(View(data.value if data else None, b, h, t))
 
 
 def _rope(**kw):
@@ -26,7 +30,7 @@ def _rope(**kw):
 
 
 def _softmax(**kw):
-    c = binding._CSoftmax(2, 4, 2, 8, 8, 64, 1, 0.125, 0.0, 0, None, None, None, None, None)
+    c = binding._CSoftmax(2, 4, 2, 24, 24, 64, 1, 0.125, 0.0, 0, None, None, None, None, None)
     for k, v in kw.items():
         setattr(c, k, v)
     return c
@@ -89,6 +93,13 @@ def test_softmax_views_and_workspace():
         assert call(_view(t=68), ok, FAKE, need) == -1 and call(_view(None), ok, FAKE, need) == -1
         assert call(ok, _view(t=32), FAKE, need) == -1 and call(_view(t=0), ok, FAKE, need) == -1
     assert L.softmax_attention_fwd(ctypes.byref(p), ok, ok, ok, ok, None, FAKE, 1 << 40, None, None) == -1
+    # a step splits its keys over CTAs and needs room for their parts; more than 2^22 - 64 queries, or keys of a backward pass
+    step, short = _softmax(nq=1, nk=1 << 20), _softmax(nq=1, nk=8)
+    assert L.softmax_attention_workspace_bytes(ctypes.byref(step), 0) > L.softmax_attention_workspace_bytes(ctypes.byref(short), 0) > 0
+    assert L.softmax_attention_fwd(ctypes.byref(step), ok, ok, ok, ok, FAKE, FAKE, 256, None, None) == -3
+    assert L.softmax_attention_workspace_bytes(ctypes.byref(_softmax(nq=1, nk=1 << 25)), 0) > 0
+    assert L.softmax_attention_workspace_bytes(ctypes.byref(_softmax(nq=1, nk=1 << 25)), 1) == 0
+    assert L.softmax_attention_workspace_bytes(ctypes.byref(_softmax(nq=1 << 23)), 0) == 0
 
 
 def test_binding_refuses_cpu_tensors():
