@@ -2,6 +2,7 @@
 #include <cudaTypedefs.h>
 #include <math.h>
 #include <stdint.h>
+#include <algorithm>
 
 #include "../../include/laplace_nystrom.h"
 #include "ln_host.cuh"
@@ -137,6 +138,24 @@ StepPlan plan_step(const ln_softmax* p) {
   return s;
 }
 
+// tcgen05 forward: query tiles a CTA (T), and the split of the keys over CTAs where the query tiles alone do not fill the GPU.
+struct SplitPlan { int tiles, chunk, splits; };
+SplitPlan plan_split(const ln_softmax* p) {
+  SplitPlan s;
+  s.tiles = p->nq <= 128 || p->nk <= 512 ? 1 : 2;
+  const long long heads = (long long)p->B * p->Hq, blocks = cdiv(p->nq, 128 * s.tiles), keys = cdiv(p->nk, 128);
+  s.chunk = (int)keys; s.splits = 1;
+  if (blocks * heads >= 2ll * sm_count()) return s;
+  // key tiles of all CTAs together; causal rows see half of the last nq keys
+  long long total = blocks * keys;
+  if (p->causal && !p->prefix) total -= blocks * (std::min(p->nq, p->nk) / 128) / 2;
+  long long chunk = (total * heads + 3ll * sm_count() - 1) / (3ll * sm_count());
+  if (chunk < 8) chunk = 8;
+  if (chunk >= keys) return s;
+  s.chunk = (int)chunk; s.splits = (int)((keys + chunk - 1) / chunk);
+  return s;
+}
+
 // Workspace: the documents of every 64 tokens, (backward) delta, (forward, a step) the splits' partial results.
 struct SmWork { int4 *rq, *rk; float* delta; StepPart part; size_t bytes; };
 SmWork carve_softmax(const ln_softmax* p, bool bwd, void* base) {
@@ -157,6 +176,14 @@ SmWork carve_softmax(const ln_softmax* p, bool bwd, void* base) {
     w.rk = reinterpret_cast<int4*>(c.take((size_t)p->B * cdiv(p->nk, 64) * 4));
   }
   if (bwd) w.delta = c.take((size_t)p->B * p->Hq * p->nq);
+  if (!bwd && p->dtype == LN_BF16) {
+    const SplitPlan s = plan_split(p);
+    const size_t rows = (size_t)p->B * p->Hq * p->nq * s.splits;
+    if (s.splits > 1) {
+      w.part.o = c.take(rows * p->d);
+      w.part.ml = reinterpret_cast<float2*>(c.take(rows * 2));
+    }
+  }
   w.bytes = c.off;
   return w;
 }
@@ -181,6 +208,10 @@ void softmax_docs(const SmArgs& a, const SmWork& w, cudaStream_t st) {
   if (a.doc_q) LN_LAUNCH("k_sm_docs", st, enqueue(k_sm_docs, dim3(a.tq + a.tk, a.B), 32, 0, st, a.doc_q, a.doc_k, a.nq, a.nk, a.tq, a.tk, w.rq, w.rk));
 }
 
+template <typename T> void softmax_join(const SmArgs& a, int splits, const StepPart& part, cudaStream_t st) {
+  LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<T>, dim3(cdiv((long long)a.B * a.Hq * a.nq, 4)), 128, 0, st, a, StepPlan{0, splits}, part));
+}
+
 void softmax_step(const ln_softmax* p, const SmArgs& a, const SmWork& w, cudaStream_t st) {
   const StepPlan s = plan_step(p);
   const dim3 grid(s.splits, a.B * a.Hk);
@@ -195,9 +226,7 @@ void softmax_step(const ln_softmax* p, const SmArgs& a, const SmWork& w, cudaStr
   else if (p->d == 64) f32(std::integral_constant<int, 64>());
   else f32(std::integral_constant<int, 128>());
   if (s.splits == 1) return;
-  const dim3 rows(cdiv((long long)a.B * a.Hq * a.nq, 4));
-  if (p->dtype == LN_BF16) LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<bf16>, rows, 128, 0, st, a, s, w.part));
-  else LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<float>, rows, 128, 0, st, a, s, w.part));
+  if (p->dtype == LN_BF16) softmax_join<bf16>(a, s.splits, w.part, st); else softmax_join<float>(a, s.splits, w.part, st);
 }
 
 template <typename T, int D> void softmax_fwd_simt(const SmArgs& a, cudaStream_t st) {
@@ -236,15 +265,17 @@ bool tile_map(const SmView& v, int B, int H, int n, int d, int rows, TileMap* m)
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D> int softmax_fwd_umma(const SmArgs& a, cudaStream_t st) {
+template <int D, int T> int softmax_fwd_umma(const SmArgs& a, const SplitPlan& pl, const StepPart& part, cudaStream_t st) {
   TileMap q, k, v;
   if (!tile_map(a.q, a.B, a.Hq, a.nq, a.d, 128, &q) || !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 128, &k) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 128, &v)) return LN_ERR_CUDA;
+  const SmSplit sp = {pl.chunk, pl.splits, part.o, part.ml};
   auto go = [&](auto kern) {
-    want_smem(kern, SuFwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(a.B * a.Hq, cdiv(a.nq, 256)), SU_THREADS, SuFwd<D>::kSmem, st, a, q, k, v));
+    want_smem(kern, SuFwd<D, T>::kSmem);
+    LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(a.B * a.Hq, cdiv(a.nq, T * 128), pl.splits), SuFwd<D, T>::kThreads, SuFwd<D, T>::kSmem, st, a, q, k, v, sp));
   };
-  if (a.cap > 0.f) { if (a.slopes) go(k_softmax_fwd_umma<D, true, true>); else go(k_softmax_fwd_umma<D, true, false>); }
-  else { if (a.slopes) go(k_softmax_fwd_umma<D, false, true>); else go(k_softmax_fwd_umma<D, false, false>); }
+  if (a.cap > 0.f) { if (a.slopes) go(k_softmax_fwd_umma<D, T, true, true>); else go(k_softmax_fwd_umma<D, T, true, false>); }
+  else { if (a.slopes) go(k_softmax_fwd_umma<D, T, false, true>); else go(k_softmax_fwd_umma<D, T, false, false>); }
+  if (pl.splits > 1) softmax_join<bf16>(a, pl.splits, part, st);
   return LN_OK;
 }
 
@@ -334,7 +365,11 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   if (is_step(p)) { softmax_step(p, a, w, st); return launch_ok(); }
   softmax_docs(a, w, st);
   int made = LN_OK;
-  if (p->dtype == LN_BF16) made = p->d == 128 ? softmax_fwd_umma<128>(a, st) : softmax_fwd_umma<64>(a, st);
+  if (p->dtype == LN_BF16) {
+    const SplitPlan pl = plan_split(p);
+    if (pl.tiles == 1) made = p->d == 128 ? softmax_fwd_umma<128, 1>(a, pl, w.part, st) : softmax_fwd_umma<64, 1>(a, pl, w.part, st);
+    else made = p->d == 128 ? softmax_fwd_umma<128, 2>(a, pl, w.part, st) : softmax_fwd_umma<64, 2>(a, pl, w.part, st);
+  }
   else if (p->d == 32) softmax_fwd_simt<float, 32>(a, st);
   else if (p->d == 64) softmax_fwd_simt<float, 64>(a, st);
   else softmax_fwd_simt<float, 128>(a, st);

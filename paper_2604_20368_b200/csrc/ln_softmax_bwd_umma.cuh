@@ -15,6 +15,7 @@
 
 namespace ln {
 
+constexpr int SU_THREADS = 320;
 template <int D> struct SuBwd {
   static constexpr int kX = 128 * D * 2, kY = 64 * D * 2;         // bytes of a stationary and of a moving tile
   static constexpr int kStages = 4;
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
           const float lse = KEYS ? L[k] : rowL, delta = KEYS ? Dl[k] : rowD;
           float bend = 1.f, y;
           if (CAP) {
-            const float t = sm_cap_r(x[c], sc);
+            const float t = rcp_fast(ex2(x[c] * sc.mul) + 1.f);
             bend = 4.f * t * (1.f - t);
             y = fmaf(-2.f * sc.cap2, t, sc.cap2 - lse);
           } else {

@@ -334,6 +334,7 @@ __global__ void __launch_bounds__(128) k_softmax_join(const __grid_constant__ Sm
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (row >= (long long)a.B * a.Hq * a.nq) return;
   const float2* ml = part.ml + row * pl.splits;
+  if (ml[0].y < 0.f) return;                               // a row that one CTA had whole is written already
   float top = -INFINITY;
   for (int s = lane; s < pl.splits; s += 32) top = fmaxf(top, ml[s].x);
 #pragma unroll
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(128) k_softmax_join(const __grid_constant__ Sm
       const float* o = part.o + (row * pl.splits + s0 + s) * a.d;
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (q * 32 < a.d) acc[q] = fmaf(ws, o[q * 32 + lane], acc[q]);
+        if (q * 32 < a.d && ws != 0.f) acc[q] = fmaf(ws, o[q * 32 + lane], acc[q]);   // a part of nothing holds nothing
     }
   }
   const int i = (int)(row % a.nq), h = (int)(row / a.nq % a.Hq), b = (int)(row / a.nq / a.Hq);

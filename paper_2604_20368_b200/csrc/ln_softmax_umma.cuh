@@ -1,24 +1,67 @@
 // Softmax attention on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 storage, forward.
 //
-// One CTA = two tiles of 128 queries of one head; the keys stream through shared memory in tiles of 128, copied by TMA.
+// One CTA = T tiles of 128 queries of one head; the keys stream through shared memory in tiles of 128, copied by TMA.
 //   S_t = Q_t K^T          (128 x 128, K = d)   both operands in shared memory, result in TMEM
 //   A_t = exp2(x - ref)    a thread owns a row: no shuffles; rounded to bf16 and written over S_t in TMEM
 //   O_t (+)= A_t V         (128 x d, K = 128)   left operand in TMEM, accumulator in TMEM
-// Warps 0-3 and 4-7 form the exponentials of tile 0 and 1, warp 8 copies, warp 9 issues the products.  While one tile's
-// exponentials are formed the tensor core works for the other tile.
+// Warps 4 t .. 4 t + 3 form the exponentials of tile t, one warp copies, one issues the products.  While one tile's exponentials
+// are formed the tensor core works for the other one: of the same CTA (T = 2: each key tile is copied once for both) or of the
+// other CTA on the SM (T = 1, for short rows, where starting and ending a CTA is most of it).
 // The reference of a row's exponentials is a maximum that is only renewed when the true one has grown by more than 8 (base 2):
 // the accumulator is then rescaled in TMEM, which is rare; A stays below 2^8, whose rounding to bf16 is the same half step, and
 // row sums are kept in 32 bits.  A enters the product rounded to bf16 (2^-8 of its value), as Q, K and V are.
-// Bound: 4 * 128 * 128 * d operations on the tensor core against 128 * 128 exponentials (16 a clock and SM; 2 more special
-// functions with a cap): at d = 128 both take 1024 clocks a tile, at d = 64 the exponentials are the longer part.
+// Key tiles come last first: with a distance bias the nearest keys then set the reference at once.
+// Bound: 4 * 128 * 128 * d operations on the tensor core (1024 clocks a tile at d = 128) against 128 * 128 exponentials at 16 a
+// clock and SM (1024 clocks; with a cap 1.25 more special functions each, see sm_cap4).  A share of the exponentials is therefore
+// formed on the FMA pipe (exp2_poly).
 #pragma once
 #include "ln_softmax.cuh"
 #include "ln_tile_umma.cuh"
 
 namespace ln {
 
-// score of a pair in base 2 from the product, the distance's share taken off; CAP: x = cap log2(e) tanh(dot scale / cap), with
-// tanh(y) = 1 - 2 / (exp(2 y) + 1): off by 2^-22 of the cap, where an approximate tanh would be off by 2^-11 of it
+__device__ __forceinline__ float max_nan(float x, float y) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ float min_nan(float x, float y) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
+// 2^x for x <= 127, at least 2^-126: round to the nearest integer by adding 1.5 * 2^23, a polynomial of degree 5 in the rest
+// (Remez fit of 2^f on [-1/2, 1/2], 7.5e-8 relative; 2.2e-7 as evaluated, the error of ex2), times the power of the integer, whose
+// bits the sum with 1.5 * 2^23 ends in.  NaN stays.  Two at a time: packed adds and multiply-adds take one issue slot for both.
+__device__ __forceinline__ void exp2_poly(float& x0, float& x1) {
+  const f32x2 x = pack2(max_nan(x0, -126.f), max_nan(x1, -126.f));
+  const f32x2 t = add2(x, pack2(12582912.f, 12582912.f));
+  const f32x2 f = fma2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), x);
+  f32x2 p = fma2(f, pack2(1.32764725e-3f, 1.32764725e-3f), pack2(9.67554096e-3f, 9.67554096e-3f));
+  p = fma2(p, f, pack2(5.55071309e-2f, 5.55071309e-2f));
+  p = fma2(p, f, pack2(2.40221202e-1f, 2.40221202e-1f));
+  p = fma2(p, f, pack2(6.93146944e-1f, 6.93146944e-1f));
+  p = fma2(p, f, pack2(1.00000012f, 1.00000012f));
+  float t0, t1;
+  unpack2(t, t0, t1);
+  p = mul2(p, pack2(__int_as_float((__float_as_int(t0) << 23) + 0x3f800000), __int_as_float((__float_as_int(t1) << 23) + 0x3f800000)));
+  unpack2(p, x0, x1);
+}
+// Four exponentials, FMA of them (0, 2 or 4) on the FMA pipe.  A masked score is -infinity: exactly 0 from ex2, 2^-126 from the
+// polynomial, which is why masked tiles take ex2 alone.
+template <int FMA> __device__ __forceinline__ void exp2_mix(float (&x)[4]) {
+  if (FMA == 4) { exp2_poly(x[0], x[1]); exp2_poly(x[2], x[3]); return; }
+  x[0] = ex2(x[0]); x[1] = ex2(x[1]);
+  if (FMA == 2) exp2_poly(x[2], x[3]);
+  else { x[2] = ex2(x[2]); x[3] = ex2(x[3]); }
+}
+
+// Scores in base 2 from the products of scale and cap.  With a cap x = cap log2(e) tanh(y), y = dot scale / cap, and
+// tanh(y) = 1 - 2 r, r = 1 / (exp(2 y) + 1): off by 2^-22 of the cap (an approximate tanh would be off by 2^-11 of it), and
+// 1 - tanh(y)^2 = 4 r (1 - r).
+// Of every four exponentials of a tile that the masks leave whole, so many on the FMA pipe: SU_FMA_EXP without a cap, with one SU_FMA_CAP of those of the
+// cap and SU_FMA_EXP_CAP of the others.
+#ifndef SU_FMA_EXP
+#define SU_FMA_EXP 2
+#endif
+#ifndef SU_FMA_CAP
+#define SU_FMA_CAP 2
+#endif
+#ifndef SU_FMA_EXP_CAP
+#define SU_FMA_EXP_CAP 2
+#endif
 struct SmScore { float mul, cap2, slope2; };
 __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
   SmScore s;
@@ -28,14 +71,25 @@ __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
   return s;
 }
 __device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-// r = 1 / (exp(2 y) + 1); tanh(y) = 1 - 2 r, 1 - tanh(y)^2 = 4 r (1 - r)
-__device__ __forceinline__ float sm_cap_r(float dot, const SmScore& s) { return rcp_fast(ex2(dot * s.mul) + 1.f); }
+// dot products -> r, four at a time with one reciprocal: 1 / u = v / (u v).  exp(2 y) is held at 2^30 (r = 2^-30 there, tanh = 1 to
+// 2^-29), so that a product of four stays in range.  One NaN makes all four NaN: masked products have to be cleared before.
+template <int FMA> __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = min_nan(x[k] * mul, 30.f);
+  exp2_mix<FMA>(x);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] += 1.f;
+  const float u = x[0] * x[1], v = x[2] * x[3], r = rcp_fast(u * v), ru = r * v, rv = r * u;
+  const float r0 = ru * x[1], r1 = ru * x[0], r2 = rv * x[3], r3 = rv * x[2];
+  x[0] = r0; x[1] = r1; x[2] = r2; x[3] = r3;
+}
 
-constexpr int SU_THREADS = 320;
-template <int D> struct SuFwd {
+template <int D, int T> struct SuFwd {
   static constexpr int kTile = 128 * D * 2;                       // bytes of a 128-row tile
-  static constexpr int kStages = D == 64 ? 4 : 2;
-  static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages);
+  static constexpr int kStages = T == 1 ? (D == 64 ? 2 : 1) : (D == 64 ? 4 : 2);
+  static constexpr int kThreads = T * 128 + 64, kCtas = T == 1 ? 2 : 1;
+  static constexpr int kTmem = T == 1 ? 256 : 512;
+  static constexpr size_t kSmem = 1024 + (size_t)kTile * (T + 2 * kStages);
 };
 
 // Rows r of a tile with keep(r) false become zeros (a whole warp; a row stays within its 128 bytes under the swizzle).
@@ -50,48 +104,60 @@ template <int D, typename F> __device__ __forceinline__ void tile_clear(char* ti
   __syncwarp();
 }
 
-// x[0..31] of a row, keys j0 + c0 ..: -infinity where the masks leave nothing (lim: the row's limit minus j0 + c0)
-__device__ __forceinline__ void sm_mask32(float* x, int lim, const int* dk, int doc, int j, int nk) {
-#pragma unroll
-  for (int e = 0; e < 32; ++e)
-    if (e >= lim) x[e] = -INFINITY;
-  if (dk) {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const int id = j + e < nk ? __ldg(dk + j + e) : -1;          // the same address for the whole warp
-      if (id != doc) x[e] = -INFINITY;
-    }
-  }
-}
-
 // A bounded wait whose outcome is the same in every lane.
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, umma::mbar_wait(bar, parity)); }
 
-template <int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mq,
-                                                                  const __grid_constant__ TileMap mk, const __grid_constant__ TileMap mv) {
+// The 32 moving tokens from j that the masks leave a row, as bits: [from, to), and those of its document.
+__device__ __forceinline__ uint32_t sm_left(int from, int to, const int* dm, int doc, int j, int n) {
+  from = max(from - j, 0); to = min(max(to - j, 0), 32);
+  uint32_t left = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & (from < 32 ? 0xffffffffu << from : 0u);
+  if (dm)
+#pragma unroll 8
+    for (int e = 0; e < 32; ++e) {
+      const int id = j + e < n ? __ldg(dm + j + e) : -1;          // the same address for the whole warp
+      if (id != doc) left &= ~(1u << e);
+    }
+  return left;
+}
+
+// Keys are split over CTAs (blockIdx.z) where the query tiles alone do not fill the GPU: a CTA takes `chunk` of its key tiles.
+struct SmSplit { int chunk, splits; float* o; float2* ml; };       // parts: [row][split][d], maximum (base 2) and sum
+
+template <int D, int T, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(SuFwd<D, T>::kThreads, SuFwd<D, T>::kCtas)
+k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk,
+                   const __grid_constant__ TileMap mv, const __grid_constant__ SmSplit sp) {
   pdl_wait();
-  constexpr int NS = SuFwd<D>::kStages, TB = SuFwd<D>::kTile;
+  constexpr int NS = SuFwd<D, T>::kStages, TB = SuFwd<D, T>::kTile, COPY = 4 * T, MMA = 4 * T + 1, TMEM = SuFwd<D, T>::kTmem, TO = T * 128;
   extern __shared__ __align__(16) char su_smem[];
   char* base = su_smem + ((1024u - (umma::s32(su_smem) & 1023u)) & 1023u);
-  char *sQ = base, *sK = base + 2 * TB, *sV = sK + NS * TB;
-  __shared__ unsigned long long q_full, k_full[NS], k_free[NS], v_full[NS], v_free[NS], v_raw, s_full[2], p_ready[2], o_full[2], spare;
+  char *sQ = base, *sK = base + T * TB, *sV = sK + NS * TB;
+  __shared__ unsigned long long q_full, k_full[NS], k_free[NS], v_full[NS], v_free[NS], v_raw, s_full[T], p_ready[T], o_full[T], spare;
   __shared__ uint32_t tmem_slot;
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int bh = blockIdx.x, b = bh / a.Hq, h = bh % a.Hq, hk = h / a.group;
-  const int i0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * 256;                 // long causal rows first
+  const int i0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * (T * 128);           // long causal rows first
   const SmMask m(a, b);
-  const int2 range = sm_range<256, false>(a, m, b, i0, sh);
-  const int nt = (range.y - range.x + 1) / 2, k0 = range.x * 64;             // key tiles of 128 from k0
+  const int2 range = sm_range<T * 128, false>(a, m, b, i0, sh);
+  // key tiles of 128 from k0, the last one first
+  const int all = (range.y - range.x + 1) / 2, z0 = sp.splits > 1 ? (int)blockIdx.z * sp.chunk : 0;
+  const int nt = sp.splits > 1 ? min(max(all - z0, 0), sp.chunk) : all, k0 = range.x * 64 + z0 * 128;
+  const bool alone = sp.splits == 1 || all <= sp.chunk;                        // this CTA has all keys of its rows
+  if (sp.splits > 1 && blockIdx.z && nt == 0) {                                // nothing for this split: a part of nothing
+    if (!alone)
+      for (int r = tid; r < T * 128 && i0 + r < a.nq; r += SuFwd<D, T>::kThreads)
+        sp.ml[((long long)bh * a.nq + i0 + r) * sp.splits + blockIdx.z] = make_float2(-INFINITY, 0.f);
+    return;
+  }
   if (tid == 0) {
     umma::mbar_init(&q_full, 1); umma::mbar_init(&v_raw, 1); umma::mbar_init(&spare, 1);
     for (int s = 0; s < NS; ++s) {
       umma::mbar_init(&k_full[s], 1); umma::mbar_init(&k_free[s], 1); umma::mbar_init(&v_full[s], 1); umma::mbar_init(&v_free[s], 1);
     }
-    for (int t = 0; t < 2; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); umma::mbar_init(&o_full[t], 1); }
+    for (int t = 0; t < T; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); umma::mbar_init(&o_full[t], 1); }
   }
-  if (warp == 9) umma::tmem_alloc(&tmem_slot, 512);
+  if (warp == MMA) umma::tmem_alloc(&tmem_slot, TMEM);
   umma::fence_before_sync();
   __syncthreads();
   umma::fence_after_sync();
@@ -99,20 +165,20 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
   const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
   bool ok = true;
 
-  if (warp == 8) {                                                           // copies
+  if (warp == COPY) {                                                        // copies
     const bool one = umma::elect_one();
     const int qh = h * mq.head, qb = b * mq.batch, kh = hk * mk.head, kb = b * mk.batch, vh = hk * mv.head, vb = b * mv.batch;
     if (nt > 0 && one) {
-      umma::mbar_expect_tx(&q_full, 2 * TB);
+      umma::mbar_expect_tx(&q_full, T * TB);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int blk = 0; blk < D / 64; ++blk)
           umma::tile_load(umma::s32(sQ) + t * TB + blk * 16384, &mq.map, blk * 64, i0 + t * 128, qh, qb, &q_full);
     }
     int raw = 0, j = 0;
     for (; j < nt && ok; ++j) {
-      const int s = j % NS, j0 = k0 + j * 128;
+      const int s = j % NS, j0 = k0 + (nt - 1 - j) * 128;
       const uint32_t again = (uint32_t)(j / NS - 1) & 1;
       if (j >= NS) ok = warp_wait(&k_free[s], again);
       if (one && ok) {
@@ -145,7 +211,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
         if (j > s) { umma::mbar_wait(&k_full[s], last & 1); umma::mbar_wait(&v_full[s], last & 1); }
         if (j % NS == s && j < nt) umma::mbar_wait(&k_full[s], (j / NS) & 1, 1 << 12);
       }
-  } else if (warp == 9) {                                                    // products
+  } else if (warp == MMA) {                                                  // products
     if (umma::elect_one() && nt > 0) {
       const uint32_t id_s = umma::instr_desc(128, false, false), id_o = umma::instr_desc(D, false, true);
       const int steps = a.d / 16;
@@ -157,19 +223,23 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
       };
       ok = umma::mbar_wait(&q_full, 0) && umma::mbar_wait(&k_full[0], 0);
       umma::fence_after_sync();
-      if (ok) { scores(0, 0); scores(1, 0); if (NS < nt) umma::commit(&k_free[0]); }
+      if (ok) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) scores(t, 0);
+        if (NS < nt) umma::commit(&k_free[0]);
+      }
       for (int j = 0; j < nt && ok; ++j) {
         const int s = j % NS, s1 = (j + 1) % NS;
         ok = umma::mbar_wait(&v_full[s], (j / NS) & 1);
         if (ok && j + 1 < nt) ok = umma::mbar_wait(&k_full[s1], ((j + 1) / NS) & 1);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < T; ++t) {
           ok = ok && umma::mbar_wait(&p_ready[t], j & 1);
           if (!ok) break;
           umma::fence_after_sync();
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks)
-            umma::mma_ta(tm + 256 + t * D, tm + t * 128 + ks * 8, umma::cols_desc(va + s * TB, 128, ks), id_o, j > 0 || ks > 0);
+            umma::mma_ta(tm + TO + t * D, tm + t * 128 + ks * 8, umma::cols_desc(va + s * TB, 128, ks), id_o, j > 0 || ks > 0);
           if (j + 1 < nt) scores(t, s1);
           else umma::commit(&o_full[t]);
         }
@@ -182,41 +252,77 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
   } else {                                                                   // exponentials
     const int t = warp >> 2, lane = tid & 31, row = (warp & 3) * 32 + lane, i = i0 + t * 128 + row;
     const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tm + quarter + t * 128, to = tm + quarter + 256 + t * D;
+    const uint32_t ts = tm + quarter + t * 128, to = tm + quarter + TO + t * D;
     const int doc = a.doc_q && i < a.nq ? a.doc_q[(long long)b * a.nq + i] : 0;
     const int lim = i < a.nq && doc >= 0 ? m.limit(i) : 0;
     const SmScore sc = sm_score_of(a, h);
     float ref = -INFINITY, sum = 0.f;
     for (int j = 0; j < nt; ++j) {
-      const int j0 = k0 + j * 128;
+      const int j0 = k0 + (nt - 1 - j) * 128;
       const bool whole = sm_whole(a, m, b, i0 + t * 128, i0 + t * 128 + 128, j0, j0 + 128);
+      uint32_t left[4];
+      if (!whole)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) left[c] = sm_left(0, lim, dk, doc, j0 + c * 32, a.nk);
       ok = warp_wait(&s_full[t], j & 1);
       if (!ok) break;
       umma::fence_after_sync();
-      float x[128];
+      // first pass over the row: its maximum.  With a bias the scores are formed here and go back to TMEM; a cap alone does not
+      // move the maximum to another key.
+      float x[2][32];
+      float mx = -INFINITY;
+      umma::tmem_ld32_async(ts, x[0]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) umma::tmem_ld32_async(ts + c * 32, x + c * 32);
-      umma::tmem_ld_wait();
+      for (int c = 0; c < 4; ++c) {
+        float* v = x[c & 1];
+        umma::tmem_ld_wait();
+        umma::tie32(v);
+        if (c < 3) umma::tmem_ld32_async(ts + c * 32 + 32, x[(c + 1) & 1]);
+        if (BIAS) {
+          if (CAP) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) umma::tie32(x + c * 32);
-      if (CAP) {
+            for (int e = 0; e < 32; e += 4) {
+              float q[4];
 #pragma unroll
-        for (int e = 0; e < 128; ++e) x[e] = fmaf(-2.f * sc.cap2, sm_cap_r(x[e], sc), sc.cap2);
+              for (int k = 0; k < 4; ++k) q[k] = !whole && !((left[c] >> (e + k)) & 1u) ? 0.f : v[e + k];
+              sm_cap4<SU_FMA_CAP>(q, sc.mul);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[e + k] = q[k];
+            }
+          }
+          const float p = (float)(i + m.off - j0 - c * 32);
+          uint32_t w[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float far = sc.slope2 * fabsf(p - (float)e);
+            v[e] = CAP ? fmaf(-2.f * sc.cap2, v[e], sc.cap2 - far) : fmaf(v[e], sc.mul, -far);
+            if (!whole && !((left[c] >> e) & 1u)) v[e] = -INFINITY;
+            w[e] = __float_as_uint(v[e]);
+          }
+          umma::tmem_st32(ts + c * 32, w);
+        } else if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (!((left[c] >> e) & 1u)) v[e] = -INFINITY;
+        }
+        float top[2] = {fmaxf(v[0], v[1]), fmaxf(v[2], v[3])};
+#pragma unroll
+        for (int e = 4; e < 32; e += 4) {
+          top[0] = fmaxf(fmaxf(top[0], v[e]), v[e + 1]);
+          top[1] = fmaxf(fmaxf(top[1], v[e + 2]), v[e + 3]);
+        }
+        mx = fmaxf(fmaxf(mx, top[0]), top[1]);
       }
-      if (BIAS) {
-        const float p = (float)(i + m.off - j0);
-#pragma unroll
-        for (int e = 0; e < 128; ++e) x[e] = fmaf(-sc.slope2, fabsf(p - (float)e), CAP ? x[e] : x[e] * sc.mul);
+      if (BIAS) umma::tmem_st_wait();
+      umma::tmem_ld32_async(ts, x[0]);
+      if (!BIAS) {                                                           // scale > 0: the largest product is the largest score
+        if (CAP) {
+          const float r = rcp_fast(ex2(fminf(mx * sc.mul, 30.f)) + 1.f);
+          mx = mx == -INFINITY ? mx : fmaf(-2.f * sc.cap2, r, sc.cap2);
+        } else {
+          mx *= sc.mul;
+        }
       }
-      if (!whole) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) sm_mask32(x + c * 32, lim - j0 - c * 32, dk, doc, j0 + c * 32, a.nk);
-      }
-      float top[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-      for (int e = 4; e < 128; ++e) top[e & 3] = fmaxf(top[e & 3], x[e]);
-      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      if (!(CAP || BIAS)) mx *= sc.mul;                                      // scale > 0: the largest product is the largest score
       const bool grown = mx > ref + 8.f;                                     // also the first finite maximum of a row
       if (__any_sync(0xffffffffu, grown)) {
         const float now = grown ? mx : ref;
@@ -226,32 +332,59 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
         if (j > 0) {                                                         // every product into O is complete (s_full follows them)
 #pragma unroll
           for (int c = 0; c < D; c += 32) {
-            float o[32];
             uint32_t w[32];
-            umma::tmem_ld32_async(to + c, o);
+            umma::tmem_ld32_async(to + c, x[1]);
             umma::tmem_ld_wait();
-            umma::tie32(o);
+            umma::tie32(x[0]);
+            umma::tie32(x[1]);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * f);
+            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(x[1][e] * f);
             umma::tmem_st32(to + c, w);
           }
         }
       }
       const float shift = ref == -INFINITY ? 0.f : -ref;
       float part[4] = {0.f, 0.f, 0.f, 0.f};
+      // second pass: exponentials, rounded and packed over the scores that were read
+      auto second = [&](auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        constexpr int F1 = MASKED ? 0 : SU_FMA_CAP, F2 = MASKED ? 0 : (CAP ? SU_FMA_EXP_CAP : SU_FMA_EXP);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t w[32];
+        for (int c = 0; c < 4; ++c) {
+          float* v = x[c & 1];
+          umma::tmem_ld_wait();
+          umma::tie32(v);
+          if (c < 3) umma::tmem_ld32_async(ts + c * 32 + 32, x[(c + 1) & 1]);
+          uint32_t w[16];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int u = c * 64 + 2 * e;
-          const float p0 = ex2(CAP || BIAS ? x[u] + shift : fmaf(x[u], sc.mul, shift));
-          const float p1 = ex2(CAP || BIAS ? x[u + 1] + shift : fmaf(x[u + 1], sc.mul, shift));
-          part[(2 * e) & 3] += p0; part[(2 * e + 1) & 3] += p1;
-          w[e] = umma::pack_bf16(p0, p1);
+          for (int e = 0; e < 32; e += 4) {
+            float q[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+            if (CAP && !BIAS) {
+              if (MASKED)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (!((left[c] >> (e + k)) & 1u)) q[k] = 0.f;
+              sm_cap4<F1>(q, sc.mul);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) q[k] = fmaf(-2.f * sc.cap2, q[k], sc.cap2 + shift);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) q[k] = BIAS ? q[k] + shift : fmaf(q[k], sc.mul, shift);
+            }
+            if (MASKED && !BIAS)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (!((left[c] >> (e + k)) & 1u)) q[k] = -INFINITY;
+            exp2_mix<F2>(q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[k] += q[k];
+            w[e / 2] = umma::pack_bf16(q[0], q[1]);
+            w[e / 2 + 1] = umma::pack_bf16(q[2], q[3]);
+          }
+          umma::tmem_st16(ts + c * 16, w);
         }
-        umma::tmem_st32(ts + c * 32, w);
-      }
+      };
+      if (whole) second(std::false_type()); else second(std::true_type());
       sum += (part[0] + part[1]) + (part[2] + part[3]);
       umma::tmem_st_wait();
       umma::fence_before_sync();
@@ -262,7 +395,20 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
       ok = ok && warp_wait(&o_full[t], 0);
       umma::fence_after_sync();
     }
-    if (ok) {
+    if (ok && !alone) {                                                      // a part: 32-bit accumulators as they are
+      float* po = sp.o + (((long long)bh * a.nq + i) * sp.splits + blockIdx.z) * a.d;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {                                      // every lane loads (the instruction is the warp's), rows in range store
+        float o[32];
+        umma::tmem_ld32_async(to + c, o);
+        umma::tmem_ld_wait();
+        umma::tie32(o);
+        if (i < a.nq && c < a.d)
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      }
+      if (i < a.nq) sp.ml[((long long)bh * a.nq + i) * sp.splits + blockIdx.z] = make_float2(ref, sum);
+    } else if (ok) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       // a warp's 32 rows go through its part of the query tile (no product reads it any more), 16-byte pieces swizzled by row
       char* stage = sQ + t * TB + (warp & 3) * 32 * D * 2;
@@ -292,13 +438,17 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_fwd_umma(const __grid
         if (first + r < a.nq)
           *reinterpret_cast<uint4*>(O + (first + r) * a.o.t + p * 8) = *reinterpret_cast<const uint4*>(stage + (r * PR + (p ^ (r & 7))) * 16);
       }
-      if (i < a.nq) a.lse[(long long)bh * a.nq + i] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+      if (i < a.nq) {
+        a.lse[(long long)bh * a.nq + i] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+        // one part, whole: the join passes over the row
+        if (sp.splits > 1) sp.ml[((long long)bh * a.nq + i) * sp.splits] = make_float2(0.f, -1.f);
+      }
     }
   }
   __syncwarp();
   umma::fence_before_sync();
   __syncthreads();
-  if (warp == 9) umma::tmem_dealloc(tm, 512);
+  if (warp == MMA) umma::tmem_dealloc(tm, TMEM);
   umma::report_timeout(ok, a.dev_status, bh);
 }
 

@@ -18,7 +18,7 @@ class View(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
 
 
-def _view(data=FAKE, b=4096, h=512, t=64):
+def _view(data=FAKE, b=16384, h=2048, t=64):
     return ctypes.byref(View(data.value if data else None, b, h, t))
 
 
@@ -54,11 +54,11 @@ def test_rope_sizes_and_views():
         assert call(*bad, ok, ok, ok, ok) == -1
     assert call(2, (1 << 30) + 1, 8, 8, ok, ok, ok, ok) == -2
     assert call(1 << 14, 1 << 14, 8, 8, ok, ok, ok, ok) == -2            # 2^32 rows
-    for bad in (_view(None), _view(NEAR), _view(t=60), _view(h=-512)):
+    for bad in (_view(None), _view(NEAR), _view(t=60), _view(h=-2048)):
         assert call(2, 8, 8, 8, bad, ok, ok, ok) == -1
         assert call(2, 8, 8, 8, ok, ok, ok, bad) == -1
     assert call(2, 8, 8, 8, ok, ok, ok, _view(h=0)) == -1                # rows of an output overlap
-    assert call(2, 8, 8, 8, ok, ok, ok, _view(b=8 * 512 - 64)) == -1
+    assert call(2, 8, 8, 8, ok, ok, ok, _view(b=7 * 2048 + 7 * 64)) == -1
     assert L.qk_norm_rope_fwd(ctypes.byref(p), 2, 8, 8, 8, -1.0, None, None, ok, ok, ok, ok, None) == -1
     assert L.qk_norm_rope_fwd(ctypes.byref(p), 2, 8, 8, 8, 1e-6, NEAR, None, ok, ok, ok, ok, None) == -1
     need = L.qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p), 2, 8, 8, 8)
