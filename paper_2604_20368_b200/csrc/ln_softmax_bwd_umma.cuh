@@ -5,9 +5,9 @@
 //   keys stationary    (KEYS true):   X1 = K, X2 = V;   Y1 = Q, Y2 = dO of every query head of the group;  dK += ds Y1, dV += A Y2
 // Per tile: S = X1 Y1^T and dP = X2 Y2^T (128 x 64, K = d, operands in shared memory), then A = exp2(x - lse) and
 // ds = A (dP - delta) (1 - tanh^2), both rounded to bf16 and written over S and dP in TMEM, from where they are the left operands
-// of the products into the accumulators (128 x d in TMEM).  S and dP are double-buffered: the tensor core forms those of the next
-// tile while this one's exponentials are formed.  Warps 0-7: warp w owns rows 32 (w % 4) .. and columns 32 (w / 4) ..; warp 8
-// copies, warp 9 issues the products.  `scale` is applied once, to the accumulators.
+// of the products into the accumulators (128 x d in TMEM).  S and dP are double-buffered: warps 0-3 form the exponentials of the
+// even tiles, warps 4-7 those of the odd ones (a thread owns a row), and while one group waits for the tensor core the other has
+// work.  Warp 8 copies, warp 9 issues the products.  `scale` is applied once, to the accumulators.
 // Two passes form S and dP twice (7 products a pair instead of 5): no atomics, and every sum has one order.
 // Bound by the tensor core's operand reads: with 64 columns a product reads 128 + 64 rows of shared memory for 128 x 64 results.
 #pragma once
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   char *sX = base, *sY = base + 2 * XB;                                      // X1, X2; per stage Y1, Y2
   __shared__ unsigned long long x_full, y_full[NS], y_free[NS], y_raw, l_full[NS], s_full[2], p_ready[2], acc_full, spare;
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(16) float sL[KEYS ? NS : 1][64], sD[KEYS ? NS : 1][64];
+  __shared__ __align__(16) float sL[KEYS ? NS : 1][64], sD[KEYS ? NS : 1][64];     // -lse (base 2) and -delta of the moving queries
   __shared__ float sDelta[KEYS ? 1 : 2][128];
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   if (tid == 0) {
     umma::mbar_init(&x_full, 1); umma::mbar_init(&y_raw, 1); umma::mbar_init(&acc_full, 1); umma::mbar_init(&spare, 1);
     for (int s = 0; s < NS; ++s) { umma::mbar_init(&y_full[s], 1); umma::mbar_init(&y_free[s], 1); umma::mbar_init(&l_full[s], 1); }
-    for (int t = 0; t < 2; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 8); }
+    for (int t = 0; t < 2; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); }
   }
   if (warp == 9) umma::tmem_alloc(&tmem_slot, 512);
   umma::fence_before_sync();
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
 #pragma unroll
         for (int u = 0; u < 64; u += 32) {
           const bool in = m0 + u + lane < a.nq;
-          sL[s][u + lane] = in ? a.lse[at + u + lane] * kLog2e : 0.f;
-          sD[s][u + lane] = in ? a.delta[at + u + lane] : 0.f;
+          sL[s][u + lane] = in ? -a.lse[at + u + lane] * kLog2e : 0.f;
+          sD[s][u + lane] = in ? -a.delta[at + u + lane] : 0.f;
         }
         __syncwarp();
         if (one) umma::mbar_arrive(&l_full[s]);
@@ -115,36 +115,39 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   } else if (warp == 9) {                                                    // products
     if (umma::elect_one() && total > 0) {
       const uint32_t id_s = umma::instr_desc(64, false, false), id_a = umma::instr_desc(D, false, true);
-      const int steps = a.d / 16;
-      const uint32_t x1 = umma::s32(sX), x2 = x1 + XB, y0 = umma::s32(sY);
-      auto scores = [&](int n) {                                             // S and dP of tile n
+      const uint64_t x1 = umma::rows_desc(umma::s32(sX)), x2 = x1 + (XB >> 4), yr = umma::rows_desc(umma::s32(sY)), yc = umma::cols_desc(umma::s32(sY), 64);
+      auto arrived = [&](int n) { ok = ok && umma::mbar_wait(&y_full[n % NS], (uint32_t)(n / NS) & 1); };
+      auto scores = [&](int n) {                                             // S and dP of tile n (d = 32: the upper channels are zeros)
         const int s = n % NS, buf = n & 1;
-        const uint32_t y1 = y0 + s * 2 * YB, y2 = y1 + YB;
-        ok = ok && umma::mbar_wait(&y_full[s], (uint32_t)(n / NS) & 1);
-        if (!ok) return;
-        umma::fence_after_sync();
-        for (int ks = 0; ks < steps; ++ks)
-          umma::mma(tm + buf * 128, umma::rows_desc(x1, 128, ks), umma::rows_desc(y1, 64, ks), id_s, ks > 0);
-        for (int ks = 0; ks < steps; ++ks)
-          umma::mma(tm + buf * 128 + 64, umma::rows_desc(x2, 128, ks), umma::rows_desc(y2, 64, ks), id_s, ks > 0);
+        const uint64_t y1 = yr + (uint64_t)(s * (2 * YB >> 4)), y2 = y1 + (YB >> 4);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) umma::mma(tm + buf * 128, x1 + umma::rows_step(128, ks), y1 + umma::rows_step(64, ks), id_s, ks > 0);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) umma::mma(tm + buf * 128 + 64, x2 + umma::rows_step(128, ks), y2 + umma::rows_step(64, ks), id_s, ks > 0);
         umma::commit(&s_full[buf]);
       };
       ok = umma::mbar_wait(&x_full, 0);
+      arrived(0);
       umma::fence_after_sync();
-      scores(0);
-      if (total > 1) scores(1);
+      if (ok) scores(0);
+      if (total > 1) {
+        arrived(1);
+        if (ok) scores(1);
+      }
       for (int n = 0; n < total && ok; ++n) {
         const int s = n % NS, buf = n & 1;
-        const uint32_t y1 = y0 + s * 2 * YB, y2 = y1 + YB;
-        ok = umma::mbar_wait(&p_ready[buf], (uint32_t)(n >> 1) & 1);
+        const uint64_t y1 = yc + (uint64_t)(s * (2 * YB >> 4)), y2 = y1 + (YB >> 4);
+        // a wait costs some 200 clocks beside the products' operand reads, so the one for tile n + 2 comes while this tile's
+        // exponentials are still being formed
+        if (n + 2 < total) arrived(n + 2);
+        ok = ok && umma::mbar_wait(&p_ready[buf], (uint32_t)(n >> 1) & 1);
         if (!ok) break;
         umma::fence_after_sync();
-        // a warp leaves its 32 columns in 16 packed ones at the place it read them from
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const uint32_t at = tm + buf * 128 + (ks >> 1) * 32 + (ks & 1) * 8;
-          if (KEYS) umma::mma_ta(tm + ACC1, at, umma::cols_desc(y2, 64, ks), id_a, n > 0 || ks > 0);
-          umma::mma_ta(tm + ACC2, at + 64, umma::cols_desc(y1, 64, ks), id_a, n > 0 || ks > 0);
+        for (int ks = 0; ks < 4; ++ks) {                                     // 64 columns became 32 packed ones at the front of their place
+          const uint32_t at = tm + buf * 128 + ks * 8;
+          if (KEYS) umma::mma_ta(tm + ACC1, at, y2 + umma::cols_step(ks), id_a, n > 0 || ks > 0);
+          umma::mma_ta(tm + ACC2, at + 64, y1 + umma::cols_step(ks), id_a, n > 0 || ks > 0);
         }
         if (n + NS < total) umma::commit(&y_free[s]);                        // only where the copying warp waits for it
         if (n + 2 < total) scores(n + 2);
@@ -181,68 +184,87 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
       if (half == 0 && r < a.nq) a.delta[at] = rowD;
     }
     const int* dm = KEYS ? dq : dk;
-    const int nm = KEYS ? a.nq : a.nk;
-    for (int n = 0; n < total; ++n) {
-      const int buf = n & 1, s = n % NS, m0 = (range.x + n % nt) * 64, c0 = half * 32;
-      const SmScore sc = sm_score_of(a, first_head + n / nt);
+    const int nm = KEYS ? a.nq : a.nk, buf = half;
+    SmScore sc = sm_score_of(a, first_head);
+    const f32x2 ka = pack2(CAP ? -2.f * sc.cap2 : sc.mul, CAP ? -2.f * sc.cap2 : sc.mul), kb = pack2(sc.cap2, sc.cap2);
+    const f32x2 rowL2 = pack2(-rowL, -rowL), rowD2 = pack2(-rowD, -rowD);
+    const uint32_t ts = tm + quarter + buf * 128;
+    int tile = range.x + half, head = first_head;                            // of moving tile n
+    uint32_t turn = 0;                                                       // how often this group has waited for its buffer
+    for (int n = half; n < total; n += 2, ++turn) {
+      while (tile >= range.x + nt) {                                         // the next query head of the group
+        tile -= nt; ++head;
+        if (BIAS) sc.slope2 = a.slopes[head] * kLog2e;
+      }
+      const int s = n % NS, m0 = tile * 64;
+      tile += 2;
       const bool whole = KEYS ? s0 + 128 <= a.nk && sm_whole(a, m, b, m0, m0 + 64, s0, s0 + 128) : sm_whole(a, m, b, s0, s0 + 128, m0, m0 + 64);
-      const uint32_t ts = tm + quarter + buf * 128 + c0;
-      ok = (!KEYS || warp_wait(&l_full[s], (uint32_t)(n / NS) & 1)) && warp_wait(&s_full[buf], (uint32_t)(n >> 1) & 1);
+      ok = (!KEYS || warp_wait(&l_full[s], (uint32_t)(n / NS) & 1)) && warp_wait(&s_full[buf], turn & 1);
       if (!ok) break;
       umma::fence_after_sync();
-      float x[32], g[32];
-      umma::tmem_ld32_async(ts, x);
-      umma::tmem_ld32_async(ts + 64, g);
-      umma::tmem_ld_wait();
-      umma::tie32(x);
-      umma::tie32(g);
-      uint32_t left = 0xffffffffu;                                           // columns that the masks leave
-      if (!whole) {
-        const int from = max(lo - m0 - c0, 0), to = min(max(hi - m0 - c0, 0), 32);
-        left = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & (from < 32 ? 0xffffffffu << from : 0u);
-        if (dm)
-#pragma unroll 4
-          for (int e = 0; e < 32; ++e) {
-            const int j = m0 + c0 + e, id = j < nm ? __ldg(dm + j) : -1;     // the same address for the whole warp
-            if (id != doc) left &= ~(1u << e);
+      // 32 columns at a time; what the masks leave out is 0 in A and ds, whatever the products are
+      auto columns = [&](int c0, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        float x[32], g[32];
+        umma::tmem_ld32_async(ts + c0, x);
+        umma::tmem_ld32_async(ts + 64 + c0, g);
+        const uint32_t left = MASKED ? sm_left(lo, hi, dm, doc, m0 + c0, nm) : 0xffffffffu;
+        const float away = (float)(KEYS ? m0 + c0 + m.off - r : r + m.off - m0 - c0);   // position of the query less the key's, column 0
+        umma::tmem_ld_wait();
+        umma::tie32(x);
+        umma::tie32(g);
+        uint32_t wp[16], wd[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          f32x2 L[2] = {rowL2, rowL2}, Dl[2] = {rowD2, rowD2}, bend[2];
+          if (KEYS) {
+            const ulonglong2 u = *reinterpret_cast<const ulonglong2*>(&sL[s][c0 + e]), v = *reinterpret_cast<const ulonglong2*>(&sD[s][c0 + e]);
+            L[0] = u.x; L[1] = u.y; Dl[0] = v.x; Dl[1] = v.y;
           }
-      }
-      const float away = (float)(KEYS ? m0 + c0 + m.off - r : r + m.off - m0 - c0);   // position of the query less the key's, column 0
-      uint32_t wp[16], wd[16];
-#pragma unroll
-      for (int e = 0; e < 32; e += 4) {
-        float L[4], Dl[4];
-        if (KEYS) {
-          const float4 u = *reinterpret_cast<const float4*>(&sL[s][c0 + e]), v = *reinterpret_cast<const float4*>(&sD[s][c0 + e]);
-          L[0] = u.x; L[1] = u.y; L[2] = u.z; L[3] = u.w;
-          Dl[0] = v.x; Dl[1] = v.y; Dl[2] = v.z; Dl[3] = v.w;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int c = e + k;
-          const float lse = KEYS ? L[k] : rowL, delta = KEYS ? Dl[k] : rowD;
-          float bend = 1.f, y;
+          float q[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
           if (CAP) {
-            const float t = rcp_fast(ex2(x[c] * sc.mul) + 1.f);
-            bend = 4.f * t * (1.f - t);
-            y = fmaf(-2.f * sc.cap2, t, sc.cap2 - lse);
-          } else {
-            y = fmaf(x[c], sc.mul, -lse);
-          }
-          if (BIAS) y = fmaf(-sc.slope2, fabsf(away + (KEYS ? (float)c : -(float)c)), y);
-          float p = ex2(y), d = p * (g[c] - delta);
-          if (CAP) d *= bend;
-          if (!whole && !((left >> c) & 1u)) p = d = 0.f;
-          x[c] = p; g[c] = d;
-        }
-      }
+            if (MASKED)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        if (KEYS) wp[e] = umma::pack_bf16(x[2 * e], x[2 * e + 1]);
-        wd[e] = umma::pack_bf16(g[2 * e], g[2 * e + 1]);
+              for (int k = 0; k < 4; ++k)
+                if (!((left >> (e + k)) & 1u)) q[k] = 0.f;
+            sm_cap4(q, sc.mul);
+          }
+          float p[4], d[4];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const f32x2 v = pack2(q[2 * k], q[2 * k + 1]);
+            if (CAP) bend[k] = mul2(v, fma2(v, pack2(-4.f, -4.f), pack2(4.f, 4.f)));
+            unpack2(fma2(v, ka, CAP ? add2(kb, L[k]) : L[k]), p[2 * k], p[2 * k + 1]);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (BIAS) p[k] = fmaf(-sc.slope2, fabsf(away + (KEYS ? (float)(e + k) : -(float)(e + k))), p[k]);
+            if (MASKED && !((left >> (e + k)) & 1u)) p[k] = -INFINITY;
+            p[k] = ex2(p[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            f32x2 v = mul2(pack2(p[2 * k], p[2 * k + 1]), add2(pack2(g[e + 2 * k], g[e + 2 * k + 1]), Dl[k]));
+            if (CAP) v = mul2(v, bend[k]);
+            unpack2(v, d[2 * k], d[2 * k + 1]);
+          }
+          if (MASKED)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (!((left >> (e + k)) & 1u)) d[k] = 0.f;
+          if (KEYS) { wp[e / 2] = umma::pack_bf16(p[0], p[1]); wp[e / 2 + 1] = umma::pack_bf16(p[2], p[3]); }
+          wd[e / 2] = umma::pack_bf16(d[0], d[1]); wd[e / 2 + 1] = umma::pack_bf16(d[2], d[3]);
+        }
+        if (KEYS) umma::tmem_st16(ts + c0 / 2, wp);
+        umma::tmem_st16(ts + 64 + c0 / 2, wd);
+      };
+      if (whole) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < 64; c0 += 32) columns(c0, std::false_type());
+      } else {
+#pragma unroll 1
+        for (int c0 = 0; c0 < 64; c0 += 32) columns(c0, std::true_type());
       }
-      if (KEYS) umma::tmem_st16(ts, wp);
-      umma::tmem_st16(ts + 64, wd);
       umma::tmem_st_wait();
       umma::fence_before_sync();
       __syncwarp();

@@ -12,56 +12,17 @@
 // row sums are kept in 32 bits.  A enters the product rounded to bf16 (2^-8 of its value), as Q, K and V are.
 // Key tiles come last first: with a distance bias the nearest keys then set the reference at once.
 // Bound: 4 * 128 * 128 * d operations on the tensor core (1024 clocks a tile at d = 128) against 128 * 128 exponentials at 16 a
-// clock and SM (1024 clocks; with a cap 1.25 more special functions each, see sm_cap4).  A share of the exponentials is therefore
-// formed on the FMA pipe (exp2_poly).
+// clock and SM (1024 clocks; with a cap 1.25 more special functions each, see sm_cap4).
 #pragma once
 #include "ln_softmax.cuh"
 #include "ln_tile_umma.cuh"
 
 namespace ln {
 
-__device__ __forceinline__ float max_nan(float x, float y) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
 __device__ __forceinline__ float min_nan(float x, float y) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
-// 2^x for x <= 127, at least 2^-126: round to the nearest integer by adding 1.5 * 2^23, a polynomial of degree 5 in the rest
-// (Remez fit of 2^f on [-1/2, 1/2], 7.5e-8 relative; 2.2e-7 as evaluated, the error of ex2), times the power of the integer, whose
-// bits the sum with 1.5 * 2^23 ends in.  NaN stays.  Two at a time: packed adds and multiply-adds take one issue slot for both.
-__device__ __forceinline__ void exp2_poly(float& x0, float& x1) {
-  const f32x2 x = pack2(max_nan(x0, -126.f), max_nan(x1, -126.f));
-  const f32x2 t = add2(x, pack2(12582912.f, 12582912.f));
-  const f32x2 f = fma2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), x);
-  f32x2 p = fma2(f, pack2(1.32764725e-3f, 1.32764725e-3f), pack2(9.67554096e-3f, 9.67554096e-3f));
-  p = fma2(p, f, pack2(5.55071309e-2f, 5.55071309e-2f));
-  p = fma2(p, f, pack2(2.40221202e-1f, 2.40221202e-1f));
-  p = fma2(p, f, pack2(6.93146944e-1f, 6.93146944e-1f));
-  p = fma2(p, f, pack2(1.00000012f, 1.00000012f));
-  float t0, t1;
-  unpack2(t, t0, t1);
-  p = mul2(p, pack2(__int_as_float((__float_as_int(t0) << 23) + 0x3f800000), __int_as_float((__float_as_int(t1) << 23) + 0x3f800000)));
-  unpack2(p, x0, x1);
-}
-// Four exponentials, FMA of them (0, 2 or 4) on the FMA pipe.  A masked score is -infinity: exactly 0 from ex2, 2^-126 from the
-// polynomial, which is why masked tiles take ex2 alone.
-template <int FMA> __device__ __forceinline__ void exp2_mix(float (&x)[4]) {
-  if (FMA == 4) { exp2_poly(x[0], x[1]); exp2_poly(x[2], x[3]); return; }
-  x[0] = ex2(x[0]); x[1] = ex2(x[1]);
-  if (FMA == 2) exp2_poly(x[2], x[3]);
-  else { x[2] = ex2(x[2]); x[3] = ex2(x[3]); }
-}
-
 // Scores in base 2 from the products of scale and cap.  With a cap x = cap log2(e) tanh(y), y = dot scale / cap, and
 // tanh(y) = 1 - 2 r, r = 1 / (exp(2 y) + 1): off by 2^-22 of the cap (an approximate tanh would be off by 2^-11 of it), and
 // 1 - tanh(y)^2 = 4 r (1 - r).
-// Of every four exponentials of a tile that the masks leave whole, so many on the FMA pipe: SU_FMA_EXP without a cap, with one SU_FMA_CAP of those of the
-// cap and SU_FMA_EXP_CAP of the others.
-#ifndef SU_FMA_EXP
-#define SU_FMA_EXP 2
-#endif
-#ifndef SU_FMA_CAP
-#define SU_FMA_CAP 2
-#endif
-#ifndef SU_FMA_EXP_CAP
-#define SU_FMA_EXP_CAP 2
-#endif
 struct SmScore { float mul, cap2, slope2; };
 __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
   SmScore s;
@@ -73,12 +34,11 @@ __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
 __device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 // dot products -> r, four at a time with one reciprocal: 1 / u = v / (u v).  exp(2 y) is held at 2^30 (r = 2^-30 there, tanh = 1 to
 // 2^-29), so that a product of four stays in range.  One NaN makes all four NaN: masked products have to be cleared before.
-template <int FMA> __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
+__device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) x[k] = min_nan(x[k] * mul, 30.f);
-  exp2_mix<FMA>(x);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) x[k] += 1.f;
+  for (int k = 0; k < 4; ++k) x[k] = ex2(x[k]) + 1.f;
   const float u = x[0] * x[1], v = x[2] * x[3], r = rcp_fast(u * v), ru = r * v, rv = r * u;
   const float r0 = ru * x[1], r1 = ru * x[0], r2 = rv * x[3], r3 = rv * x[2];
   x[0] = r0; x[1] = r1; x[2] = r2; x[3] = r3;
@@ -214,11 +174,11 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
   } else if (warp == MMA) {                                                  // products
     if (umma::elect_one() && nt > 0) {
       const uint32_t id_s = umma::instr_desc(128, false, false), id_o = umma::instr_desc(D, false, true);
-      const int steps = a.d / 16;
-      const uint32_t qa = umma::s32(sQ), ka = umma::s32(sK), va = umma::s32(sV);
-      auto scores = [&](int t, int s) {
-        for (int ks = 0; ks < steps; ++ks)
-          umma::mma(tm + t * 128, umma::rows_desc(qa + t * TB, 128, ks), umma::rows_desc(ka + s * TB, 128, ks), id_s, ks > 0);
+      const uint64_t qd = umma::rows_desc(umma::s32(sQ)), kd = umma::rows_desc(umma::s32(sK)), vd = umma::cols_desc(umma::s32(sV), 128);
+      auto scores = [&](int t, int s) {                                      // d = 32: the upper channels are zeros
+        const uint64_t q0 = qd + (uint64_t)(t * (TB >> 4)), k0 = kd + (uint64_t)(s * (TB >> 4));
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) umma::mma(tm + t * 128, q0 + umma::rows_step(128, ks), k0 + umma::rows_step(128, ks), id_s, ks > 0);
         umma::commit(&s_full[t]);
       };
       ok = umma::mbar_wait(&q_full, 0) && umma::mbar_wait(&k_full[0], 0);
@@ -237,9 +197,9 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
           ok = ok && umma::mbar_wait(&p_ready[t], j & 1);
           if (!ok) break;
           umma::fence_after_sync();
+          const uint64_t v0 = vd + (uint64_t)(s * (TB >> 4));
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            umma::mma_ta(tm + TO + t * D, tm + t * 128 + ks * 8, umma::cols_desc(va + s * TB, 128, ks), id_o, j > 0 || ks > 0);
+          for (int ks = 0; ks < 8; ++ks) umma::mma_ta(tm + TO + t * D, tm + t * 128 + ks * 8, v0 + umma::cols_step(ks), id_o, j > 0 || ks > 0);
           if (j + 1 < nt) scores(t, s1);
           else umma::commit(&o_full[t]);
         }
@@ -267,62 +227,49 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
       ok = warp_wait(&s_full[t], j & 1);
       if (!ok) break;
       umma::fence_after_sync();
-      // first pass over the row: its maximum.  With a bias the scores are formed here and go back to TMEM; a cap alone does not
-      // move the maximum to another key.
-      float x[2][32];
-      float mx = -INFINITY;
-      umma::tmem_ld32_async(ts, x[0]);
+      float x[128];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float* v = x[c & 1];
-        umma::tmem_ld_wait();
-        umma::tie32(v);
-        if (c < 3) umma::tmem_ld32_async(ts + c * 32 + 32, x[(c + 1) & 1]);
-        if (BIAS) {
-          if (CAP) {
+      for (int c = 0; c < 4; ++c) umma::tmem_ld32_async(ts + c * 32, x + c * 32);
+      umma::tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              float q[4];
+      for (int c = 0; c < 4; ++c) umma::tie32(x + c * 32);
+      // x: products, r of the cap, or scores with a bias; the score in base 2 is x ka + kb
+      const float ka = BIAS ? 1.f : (CAP ? -2.f * sc.cap2 : sc.mul), kb = CAP && !BIAS ? sc.cap2 : 0.f;
+      if (CAP) {
+        if (!whole)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) q[k] = !whole && !((left[c] >> (e + k)) & 1u) ? 0.f : v[e + k];
-              sm_cap4<SU_FMA_CAP>(q, sc.mul);
+          for (int e = 0; e < 128; ++e)
+            if (!((left[e >> 5] >> (e & 31)) & 1u)) x[e] = 0.f;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[e + k] = q[k];
-            }
-          }
-          const float p = (float)(i + m.off - j0 - c * 32);
-          uint32_t w[32];
+        for (int e = 0; e < 128; e += 4) {
+          float q[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
+          sm_cap4(q, sc.mul);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float far = sc.slope2 * fabsf(p - (float)e);
-            v[e] = CAP ? fmaf(-2.f * sc.cap2, v[e], sc.cap2 - far) : fmaf(v[e], sc.mul, -far);
-            if (!whole && !((left[c] >> e) & 1u)) v[e] = -INFINITY;
-            w[e] = __float_as_uint(v[e]);
-          }
-          umma::tmem_st32(ts + c * 32, w);
-        } else if (!whole) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (!((left[c] >> e) & 1u)) v[e] = -INFINITY;
-        }
-        float top[2] = {fmaxf(v[0], v[1]), fmaxf(v[2], v[3])};
-#pragma unroll
-        for (int e = 4; e < 32; e += 4) {
-          top[0] = fmaxf(fmaxf(top[0], v[e]), v[e + 1]);
-          top[1] = fmaxf(fmaxf(top[1], v[e + 2]), v[e + 3]);
-        }
-        mx = fmaxf(fmaxf(mx, top[0]), top[1]);
-      }
-      if (BIAS) umma::tmem_st_wait();
-      umma::tmem_ld32_async(ts, x[0]);
-      if (!BIAS) {                                                           // scale > 0: the largest product is the largest score
-        if (CAP) {
-          const float r = rcp_fast(ex2(fminf(mx * sc.mul, 30.f)) + 1.f);
-          mx = mx == -INFINITY ? mx : fmaf(-2.f * sc.cap2, r, sc.cap2);
-        } else {
-          mx *= sc.mul;
+          for (int k = 0; k < 4; ++k) x[e + k] = q[k];
         }
       }
+      if (BIAS) {
+        const float p = (float)(i + m.off - j0);
+#pragma unroll
+        for (int e = 0; e < 128; ++e) {
+          const float far = sc.slope2 * fabsf(p - (float)e);
+          x[e] = CAP ? fmaf(-2.f * sc.cap2, x[e], sc.cap2 - far) : fmaf(x[e], sc.mul, -far);
+        }
+      }
+      constexpr bool DOWN = CAP && !BIAS;                                    // the largest score has the smallest x
+      if (!whole)
+#pragma unroll
+        for (int e = 0; e < 128; ++e)
+          if (!((left[e >> 5] >> (e & 31)) & 1u)) x[e] = DOWN ? INFINITY : -INFINITY;
+      auto further = [](float u, float v) { return DOWN ? fminf(u, v) : fmaxf(u, v); };
+      float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+      for (int e = 4; e + 8 <= 124 + 4; e += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[k] = further(further(top[k], x[e + 2 * k]), x[e + 2 * k + 1]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top[k] = further(top[k], x[124 + k]);
+      const float mx = fmaf(further(further(top[0], top[1]), further(top[2], top[3])), ka, kb);
       const bool grown = mx > ref + 8.f;                                     // also the first finite maximum of a row
       if (__any_sync(0xffffffffu, grown)) {
         const float now = grown ? mx : ref;
@@ -331,61 +278,41 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         sum *= f;
         if (j > 0) {                                                         // every product into O is complete (s_full follows them)
 #pragma unroll
-          for (int c = 0; c < D; c += 32) {
-            uint32_t w[32];
-            umma::tmem_ld32_async(to + c, x[1]);
+          for (int c = 0; c < D; c += 16) {
+            float o[16];
+            uint32_t w[16];
+            umma::tmem_ld16_async(to + c, o);
             umma::tmem_ld_wait();
-            umma::tie32(x[0]);
-            umma::tie32(x[1]);
+            umma::tie16(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(x[1][e] * f);
-            umma::tmem_st32(to + c, w);
+            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * f);
+            umma::tmem_st16(to + c, w);
           }
         }
       }
-      const float shift = ref == -INFINITY ? 0.f : -ref;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-      // second pass: exponentials, rounded and packed over the scores that were read
-      auto second = [&](auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        constexpr int F1 = MASKED ? 0 : SU_FMA_CAP, F2 = MASKED ? 0 : (CAP ? SU_FMA_EXP_CAP : SU_FMA_EXP);
+      const float shift = kb + (ref == -INFINITY ? 0.f : -ref);
+      f32x2 part[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+      // exponentials, rounded and packed over the scores
+      const f32x2 ka2 = pack2(ka, ka), kb2 = pack2(shift, shift);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float* v = x[c & 1];
-          umma::tmem_ld_wait();
-          umma::tie32(v);
-          if (c < 3) umma::tmem_ld32_async(ts + c * 32 + 32, x[(c + 1) & 1]);
-          uint32_t w[16];
+      for (int c = 0; c < 128; c += 32) {
+        uint32_t w[16];
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float q[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
-            if (CAP && !BIAS) {
-              if (MASKED)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if (!((left[c] >> (e + k)) & 1u)) q[k] = 0.f;
-              sm_cap4<F1>(q, sc.mul);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) q[k] = fmaf(-2.f * sc.cap2, q[k], sc.cap2 + shift);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) q[k] = BIAS ? q[k] + shift : fmaf(q[k], sc.mul, shift);
-            }
-            if (MASKED && !BIAS)
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (!((left[c] >> (e + k)) & 1u)) q[k] = -INFINITY;
-            exp2_mix<F2>(q);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) part[k] += q[k];
-            w[e / 2] = umma::pack_bf16(q[0], q[1]);
-            w[e / 2 + 1] = umma::pack_bf16(q[2], q[3]);
-          }
-          umma::tmem_st16(ts + c * 16, w);
+        for (int e = 0; e < 32; e += 2) {
+          const f32x2 v = pack2(x[c + e], x[c + e + 1]);
+          float p0, p1;
+          unpack2(BIAS ? add2(v, kb2) : fma2(v, ka2, kb2), p0, p1);
+          p0 = ex2(p0); p1 = ex2(p1);
+          part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(p0, p1));
+          w[e / 2] = umma::pack_bf16(p0, p1);
         }
-      };
-      if (whole) second(std::false_type()); else second(std::true_type());
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
+        umma::tmem_st16(ts + c / 2, w);
+      }
+      {
+        float u0, u1;
+        unpack2(add2(part[0], part[1]), u0, u1);
+        sum += u0 + u1;
+      }
       umma::tmem_st_wait();
       umma::fence_before_sync();
       __syncwarp();

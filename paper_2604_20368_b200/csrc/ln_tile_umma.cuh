@@ -20,14 +20,13 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, uint32_t lbo_bytes
   d |= (uint64_t)2 << 61;   // 128-byte swizzle
   return d;
 }
-// K-step ks (16 channels) of a tile as a K-major operand; rows: rows of a block
-__device__ __forceinline__ uint64_t rows_desc(uint32_t tile, int rows, int ks) {
-  return tile_desc(tile + (uint32_t)(ks >> 2) * (uint32_t)rows * 128u + (uint32_t)(ks & 3) * 32u, 16);
-}
-// K-step ks (16 rows) of a tile as an MN-major operand
-__device__ __forceinline__ uint64_t cols_desc(uint32_t tile, int rows, int ks) {
-  return tile_desc(tile + (uint32_t)ks * 2048u, (uint32_t)rows * 128u);
-}
+// Descriptors of a tile as a K-major operand (rows are M or N) and as an MN-major one (rows are K, blocks of `rows` rows), and how
+// far K-step ks of it is: a constant once the loop over ks is unrolled, so that a step costs one addition.  (With the descriptor
+// formed step by step in a loop that was not unrolled an MMA was issued every 100 clocks, whatever its size.)
+__device__ __forceinline__ uint64_t rows_desc(uint32_t tile) { return tile_desc(tile, 16); }
+__device__ __forceinline__ uint64_t cols_desc(uint32_t tile, int rows) { return tile_desc(tile, (uint32_t)rows * 128u); }
+__device__ __forceinline__ constexpr uint64_t rows_step(int rows, int ks) { return (uint64_t)(((ks >> 2) * rows * 128 + (ks & 3) * 32) >> 4); }
+__device__ __forceinline__ constexpr uint64_t cols_step(int ks) { return (uint64_t)(ks * 2048 >> 4); }
 
 // D[tmem] (+)= A[tmem] * B for one K-step: A holds two bf16 of K per 32-bit column, 8 columns a step.  ONE thread.
 __device__ __forceinline__ void mma_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
@@ -47,10 +46,21 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* r) {
         "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_ld16_async(uint32_t taddr, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(taddr));
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tie32(float* r) {
 #pragma unroll
   for (int q = 0; q < 32; ++q) asm volatile("" : "+f"(r[q]));
+}
+__device__ __forceinline__ void tie16(float* r) {
+#pragma unroll
+  for (int q = 0; q < 16; ++q) asm volatile("" : "+f"(r[q]));
 }
 // 32 / 16 columns of this thread's lane <- registers
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
