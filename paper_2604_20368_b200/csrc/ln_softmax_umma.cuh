@@ -4,9 +4,11 @@
 //   S_t = Q_t K^T          (128 x 128, K = d)   both operands in shared memory, result in TMEM
 //   A_t = exp2(x - ref)    a thread owns a row: no shuffles; rounded to bf16 and written over S_t in TMEM
 //   O_t (+)= A_t V         (128 x d, K = 128)   left operand in TMEM, accumulator in TMEM
-// Warps 4 t .. 4 t + 3 form the exponentials of tile t, one warp copies, one issues the products.  While one tile's exponentials
-// are formed the tensor core works for the other one: of the same CTA (T = 2: each key tile is copied once for both) or of the
-// other CTA on the SM (T = 1, for short rows, where starting and ending a CTA is most of it).
+// Warps 4 t .. 4 t + 3 form the exponentials of tile t, one warp copies, one warp a tile issues the products (a wait costs some 200
+// clocks beside the products' operand reads, and with one warp for both tiles each waited for the other's).  While one tile's
+// exponentials are formed the tensor core works for the other one: of the same CTA (T = 2: each key tile is copied once for both)
+// or of the other CTA on the SM (T = 1, for short rows, where starting and ending a CTA is most of it).
+// With 64 channels TMEM has room for A beside S: S of the next key tile is formed as soon as this one's is in registers.
 // The reference of a row's exponentials is a maximum that is only renewed when the true one has grown by more than 8 (base 2):
 // the accumulator is then rescaled in TMEM, which is rare; A stays below 2^8, whose rounding to bf16 is the same half step, and
 // row sums are kept in 32 bits.  A enters the product rounded to bf16 (2^-8 of its value), as Q, K and V are.
@@ -47,7 +49,7 @@ __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
 template <int D, int T> struct SuFwd {
   static constexpr int kTile = 128 * D * 2;                       // bytes of a 128-row tile
   static constexpr int kStages = T == 1 ? (D == 64 ? 2 : 1) : (D == 64 ? 4 : 2);
-  static constexpr int kThreads = T * 128 + 64, kCtas = T == 1 ? 2 : 1;
+  static constexpr int kThreads = T * 160 + 32, kCtas = T == 1 ? 2 : 1;
   static constexpr int kTmem = T == 1 ? 256 : 512;
   static constexpr size_t kSmem = 1024 + (size_t)kTile * (T + 2 * kStages);
 };
@@ -88,11 +90,13 @@ __global__ void __launch_bounds__(SuFwd<D, T>::kThreads, SuFwd<D, T>::kCtas)
 k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk,
                    const __grid_constant__ TileMap mv, const __grid_constant__ SmSplit sp) {
   pdl_wait();
-  constexpr int NS = SuFwd<D, T>::kStages, TB = SuFwd<D, T>::kTile, COPY = 4 * T, MMA = 4 * T + 1, TMEM = SuFwd<D, T>::kTmem, TO = T * 128;
+  constexpr int NS = SuFwd<D, T>::kStages, TB = SuFwd<D, T>::kTile, COPY = 4 * T, MMA = 4 * T + 1, TMEM = SuFwd<D, T>::kTmem;
+  constexpr bool EARLY = D == 64;                                              // A beside S, not over it
+  constexpr int TP = EARLY ? T * 128 : 0, PC = EARLY ? 64 : 128, TO = TP + T * (EARLY ? 64 : 128);     // columns of A and O; of A a tile
   extern __shared__ __align__(16) char su_smem[];
   char* base = su_smem + ((1024u - (umma::s32(su_smem) & 1023u)) & 1023u);
   char *sQ = base, *sK = base + T * TB, *sV = sK + NS * TB;
-  __shared__ unsigned long long q_full, k_full[NS], k_free[NS], v_full[NS], v_free[NS], v_raw, s_full[T], p_ready[T], o_full[T], spare;
+  __shared__ unsigned long long q_full, k_full[NS], k_free[NS], v_full[NS], v_free[NS], v_raw, s_full[T], s_read[T], p_ready[T], o_full[T], spare[T];
   __shared__ uint32_t tmem_slot;
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -111,11 +115,13 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
     return;
   }
   if (tid == 0) {
-    umma::mbar_init(&q_full, 1); umma::mbar_init(&v_raw, 1); umma::mbar_init(&spare, 1);
+    umma::mbar_init(&q_full, 1); umma::mbar_init(&v_raw, 1);
     for (int s = 0; s < NS; ++s) {
-      umma::mbar_init(&k_full[s], 1); umma::mbar_init(&k_free[s], 1); umma::mbar_init(&v_full[s], 1); umma::mbar_init(&v_free[s], 1);
+      umma::mbar_init(&k_full[s], 1); umma::mbar_init(&k_free[s], T); umma::mbar_init(&v_full[s], 1); umma::mbar_init(&v_free[s], T);
     }
-    for (int t = 0; t < T; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); umma::mbar_init(&o_full[t], 1); }
+    for (int t = 0; t < T; ++t) {
+      umma::mbar_init(&s_full[t], 1); umma::mbar_init(&s_read[t], 4); umma::mbar_init(&p_ready[t], 4); umma::mbar_init(&o_full[t], 1); umma::mbar_init(&spare[t], 1);
+    }
   }
   if (warp == MMA) umma::tmem_alloc(&tmem_slot, TMEM);
   umma::fence_before_sync();
@@ -171,48 +177,47 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         if (j > s) { umma::mbar_wait(&k_full[s], last & 1); umma::mbar_wait(&v_full[s], last & 1); }
         if (j % NS == s && j < nt) umma::mbar_wait(&k_full[s], (j / NS) & 1, 1 << 12);
       }
-  } else if (warp == MMA) {                                                  // products
+  } else if (warp >= MMA) {                                                  // products of tile t
     if (umma::elect_one() && nt > 0) {
+      const int t = warp - MMA;
       const uint32_t id_s = umma::instr_desc(128, false, false), id_o = umma::instr_desc(D, false, true);
-      const uint64_t qd = umma::rows_desc(umma::s32(sQ)), kd = umma::rows_desc(umma::s32(sK)), vd = umma::cols_desc(umma::s32(sV), 128);
-      auto scores = [&](int t, int s) {                                      // d = 32: the upper channels are zeros
-        const uint64_t q0 = qd + (uint64_t)(t * (TB >> 4)), k0 = kd + (uint64_t)(s * (TB >> 4));
+      const uint64_t qd = umma::rows_desc(umma::s32(sQ) + t * TB), kd = umma::rows_desc(umma::s32(sK)), vd = umma::cols_desc(umma::s32(sV), 128);
+      const uint32_t ts = tm + t * 128, tp = tm + TP + t * PC, to = tm + TO + t * D;
+      auto scores = [&](int j) {                                             // d = 32: the upper channels are zeros
+        const int s = j % NS;
+        ok = ok && umma::mbar_wait(&k_full[s], (j / NS) & 1);
+        if (!ok) return;
+        umma::fence_after_sync();
+        const uint64_t k0 = kd + (uint64_t)(s * (TB >> 4));
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) umma::mma(tm + t * 128, q0 + umma::rows_step(128, ks), k0 + umma::rows_step(128, ks), id_s, ks > 0);
+        for (int ks = 0; ks < D / 16; ++ks) umma::mma(ts, qd + umma::rows_step(128, ks), k0 + umma::rows_step(128, ks), id_s, ks > 0);
         umma::commit(&s_full[t]);
-      };
-      ok = umma::mbar_wait(&q_full, 0) && umma::mbar_wait(&k_full[0], 0);
-      umma::fence_after_sync();
-      if (ok) {
-#pragma unroll
-        for (int t = 0; t < T; ++t) scores(t, 0);
-        if (NS < nt) umma::commit(&k_free[0]);
-      }
+        if (j + NS < nt) umma::commit(&k_free[s]);                           // only where the copying warp waits for it: no arrival is
+      };                                                                     // under way when the CTA ends
+      ok = umma::mbar_wait(&q_full, 0);
+      scores(0);
       for (int j = 0; j < nt && ok; ++j) {
-        const int s = j % NS, s1 = (j + 1) % NS;
-        ok = umma::mbar_wait(&v_full[s], (j / NS) & 1);
-        if (ok && j + 1 < nt) ok = umma::mbar_wait(&k_full[s1], ((j + 1) / NS) & 1);
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-          ok = ok && umma::mbar_wait(&p_ready[t], j & 1);
-          if (!ok) break;
-          umma::fence_after_sync();
-          const uint64_t v0 = vd + (uint64_t)(s * (TB >> 4));
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) umma::mma_ta(tm + TO + t * D, tm + t * 128 + ks * 8, v0 + umma::cols_step(ks), id_o, j > 0 || ks > 0);
-          if (j + 1 < nt) scores(t, s1);
-          else umma::commit(&o_full[t]);
+        const int s = j % NS;
+        if (EARLY && j + 1 < nt) {
+          ok = umma::mbar_wait(&s_read[t], j & 1);
+          scores(j + 1);
         }
-        // only where the copying warp waits for it: no arrival is under way when the CTA ends
-        if (ok && j + NS < nt) umma::commit(&v_free[s]);
-        if (ok && j + 1 + NS < nt) umma::commit(&k_free[s1]);
+        ok = ok && umma::mbar_wait(&v_full[s], (j / NS) & 1) && umma::mbar_wait(&p_ready[t], j & 1);
+        if (!ok) break;
+        umma::fence_after_sync();
+        const uint64_t v0 = vd + (uint64_t)(s * (TB >> 4));
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) umma::mma_ta(to, tp + ks * 8, v0 + umma::cols_step(ks), id_o, j > 0 || ks > 0);
+        if (EARLY || j + 1 == nt) umma::commit(&o_full[t]);
+        if (j + NS < nt) umma::commit(&v_free[s]);
+        if (!EARLY && j + 1 < nt) scores(j + 1);
       }
-      if (!ok) { umma::commit(&spare); umma::mbar_wait(&spare, 0); }          // no product is in flight when the CTA ends
+      if (!ok) { umma::commit(&spare[t]); umma::mbar_wait(&spare[t], 0); }    // no product is in flight when the CTA ends
     }
   } else {                                                                   // exponentials
     const int t = warp >> 2, lane = tid & 31, row = (warp & 3) * 32 + lane, i = i0 + t * 128 + row;
     const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tm + quarter + t * 128, to = tm + quarter + TO + t * D;
+    const uint32_t ts = tm + quarter + t * 128, tp = tm + quarter + TP + t * PC, to = tm + quarter + TO + t * D;
     const int doc = a.doc_q && i < a.nq ? a.doc_q[(long long)b * a.nq + i] : 0;
     const int lim = i < a.nq && doc >= 0 ? m.limit(i) : 0;
     const SmScore sc = sm_score_of(a, h);
@@ -233,6 +238,11 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
       umma::tmem_ld_wait();
 #pragma unroll
       for (int c = 0; c < 4; ++c) umma::tie32(x + c * 32);
+      if (EARLY) {
+        umma::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) umma::mbar_arrive(&s_read[t]);
+      }
       // x: products, r of the cap, or scores with a bias; the score in base 2 is x ka + kb
       const float ka = BIAS ? 1.f : (CAP ? -2.f * sc.cap2 : sc.mul), kb = CAP && !BIAS ? sc.cap2 : 0.f;
       if (CAP) {
@@ -270,13 +280,18 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
 #pragma unroll
       for (int k = 0; k < 4; ++k) top[k] = further(top[k], x[124 + k]);
       const float mx = fmaf(further(further(top[0], top[1]), further(top[2], top[3])), ka, kb);
+      if (EARLY && j > 0) {                                                  // A may be written, O be scaled: the product before is done
+        ok = warp_wait(&o_full[t], (j - 1) & 1);
+        if (!ok) break;
+        umma::fence_after_sync();
+      }
       const bool grown = mx > ref + 8.f;                                     // also the first finite maximum of a row
       if (__any_sync(0xffffffffu, grown)) {
         const float now = grown ? mx : ref;
         const float f = grown ? (ref == -INFINITY ? 0.f : ex2(ref - now)) : 1.f;
         ref = now;
         sum *= f;
-        if (j > 0) {                                                         // every product into O is complete (s_full follows them)
+        if (j > 0) {                                                         // every product into O is complete (else s_full follows them)
 #pragma unroll
           for (int c = 0; c < D; c += 16) {
             float o[16];
@@ -306,7 +321,7 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
           part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(p0, p1));
           w[e / 2] = umma::pack_bf16(p0, p1);
         }
-        umma::tmem_st16(ts + c / 2, w);
+        umma::tmem_st16(tp + c / 2, w);
       }
       {
         float u0, u1;
@@ -319,7 +334,7 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
       if (lane == 0) umma::mbar_arrive(&p_ready[t]);
     }
     if (nt > 0) {
-      ok = ok && warp_wait(&o_full[t], 0);
+      ok = ok && warp_wait(&o_full[t], EARLY ? (nt - 1) & 1 : 0);
       umma::fence_after_sync();
     }
     if (ok && !alone) {                                                      // a part: 32-bit accumulators as they are
