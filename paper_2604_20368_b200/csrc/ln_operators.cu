@@ -99,16 +99,14 @@ int run_qk(const ln_rope* p, int mode, float sign, int B, int n, int Hq, int Hk,
     else LN_LAUNCH("k_qk_norm_rope_bwd", st, enqueue(k_qk_rope<T, L, I, QK_NORM_BWD>, q.ctas, 256, 0, st, a));
   };
   auto lanes = [&](auto type, auto inter) {
-    switch (p->d / Piece<decltype(type)>::E) {
-      case 4: go(type, std::integral_constant<int, 4>(), inter); break;
-      case 8: go(type, std::integral_constant<int, 8>(), inter); break;
-      case 16: go(type, std::integral_constant<int, 16>(), inter); break;
-      default: go(type, std::integral_constant<int, 32>(), inter); break;
-    }
+    constexpr int E = Piece<decltype(type)>::E;
+    if (p->d == 32) go(type, std::integral_constant<int, 32 / E>(), inter);
+    else if (p->d == 64) go(type, std::integral_constant<int, 64 / E>(), inter);
+    else go(type, std::integral_constant<int, 128 / E>(), inter);
   };
   auto layout = [&](auto type) { if (p->interleaved) lanes(type, std::true_type()); else lanes(type, std::false_type()); };
   if (p->dtype == LN_F32) layout(float()); else layout(bf16());
-  if (part) LN_LAUNCH("k_gain_sum", st, enqueue(k_gain_sum, 2 * p->d / 32, 256, 0, st, part, q.ctas, p->d, dgq, dgk));
+  if (part) LN_LAUNCH("k_gain_sum", st, enqueue(k_gain_sum, 2 * p->d / 32, 1024, 0, st, part, q.ctas, p->d, dgq, dgk));
   return launch_ok();
 }
 
