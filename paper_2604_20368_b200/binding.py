@@ -7,6 +7,8 @@ loaded, or a tensor is not on a CUDA device, the call raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import math
 import os
 from dataclasses import dataclass, field
@@ -494,53 +496,38 @@ class _CSoftmax(ctypes.Structure):
                 ("slopes", ctypes.c_void_p), ("doc_q", ctypes.c_void_p), ("doc_k", ctypes.c_void_p)]
 
 
-def _launch(device, stream, call):
-    """call(raw stream) with the tensors' device as the current one and `stream` (or that device's current stream) as the
-    stream of the call, its allocations included."""
-    if device.type != "cuda":
-        raise ValueError("tensor must live on a CUDA device (there is no CPU path)")
-    if stream is None and torch.cuda.current_device() == device.index:
-        return call(torch.cuda.current_stream().cuda_stream)
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream of {stream.device} for tensors on {device}")
-    with torch.cuda.device(device):
-        if stream is None:
-            return call(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.stream(stream):
-            return call(stream.cuda_stream)
+_marshal = None
 
 
-def _heads(name, t, shape, dtype, device):
-    """Checks one [B, H, n, d] tensor; its pointer and strides, the fields of an ln_view."""
-    stride = t.stride()
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {dtype} on {device}")
-    if stride[3] != 1:
-        raise ValueError(f"{name}: the channels of a row must be adjacent")
-    return t.data_ptr(), stride[0], stride[1], stride[2]
+def marshal():
+    """The module that marshals torch tensors to the entry points below (built first if its source is newer); raises if
+    impossible."""
+    global _marshal
+    if _marshal is None:
+        path = _build.MARSHAL
+        try:
+            path = _build.build_marshal()
+        except Exception as e:   # no compiler on this machine: use the module that travelled with the tree
+            if not os.path.exists(path):
+                raise RuntimeError(f"{path} is missing and could not be built: {e}") from e
+        loader = importlib.machinery.ExtensionFileLoader("_ln_torch", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_ln_torch", loader))
+        loader.exec_module(module)
+        entries = ("rope_fwd", "rope_bwd", "qk_norm_rope_fwd", "qk_norm_rope_bwd_workspace_bytes", "qk_norm_rope_bwd",
+                   "softmax_attention_workspace_bytes", "softmax_attention_fwd", "softmax_attention_bwd")
+        module.bind({n: ctypes.cast(getattr(lib(), n), ctypes.c_void_p).value for n in entries}, LnError)
+        _marshal = module
+    return _marshal
 
 
-def _views(fields):
-    """ln_view structures one behind the other: the array that holds them, and the address of each (None for a missing tensor)."""
-    held = (ctypes.c_int64 * (4 * len(fields)))(*[x for f in fields for x in (f or (0, 0, 0, 0))])
-    at = ctypes.addressof(held)
-    return held, [None if f is None else at + 32 * i for i, f in enumerate(fields)]
-
-
-def _new(t, shape=None):
-    """An output: contiguous, whatever the strides of its model."""
-    return torch.empty(t.shape if shape is None else shape, dtype=t.dtype, device=t.device)
-
-
-def _vector(name, t, dtype, shape, device):
-    """Checks an optional contiguous tensor of the call and returns its pointer."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected a contiguous {dtype} {tuple(shape)} on {device}")
-    return t.data_ptr()
+def _on(stream, t, call, *args):
+    """call(*args) on the current stream of the tensors' device, or on `stream`, its allocations included."""
+    if stream is None:
+        return call(*args)
+    if stream.device != t.device:
+        raise ValueError(f"stream of {stream.device} for tensors on {t.device}")
+    with torch.cuda.stream(stream):
+        return call(*args)
 
 
 def rope_frequencies(r: int, base: float = 10000.0, scaling: Optional[dict] = None):
@@ -597,99 +584,34 @@ class Rope:
         # floor(2^64 frac(f / 2 pi)) in the 64-bit mantissa of x86's extended precision
         part = f.astype(np.longdouble) / _TWO_PI % 1 * np.longdouble(2) ** 64
         self.turns = torch.from_numpy(part.astype(np.uint64).view(np.int64)).to(device) if f.size else None
-
-    def c(self, like, B, n, pos, start) -> _CRope:
-        pb = pt = 0
-        if self.r and self.turns.device != like.device:
-            raise ValueError(f"Rope on {self.turns.device} for tensors on {like.device}")
-        if pos is not None:
-            if pos.dtype != torch.int32 or pos.device != like.device or pos.dim() not in (1, 2):
-                raise ValueError(f"pos: {pos.dtype} {tuple(pos.shape)} on {pos.device}, expected int32 [B, n] or [n] on {like.device}")
-            pos2 = pos[None] if pos.dim() == 1 else pos
-            if pos2.shape[1] != n or pos2.shape[0] not in (1, B):
-                raise ValueError(f"pos: shape {tuple(pos.shape)}, expected [{B}, {n}] or [{n}]")
-            pb, pt = (0 if pos2.shape[0] == 1 else pos2.stride(0)), pos2.stride(1)
-        return _CRope(self.d, self.r, int(self.interleaved), _dtype_code(like), None if not self.r else self.turns.data_ptr(),
-                      self.factor, None if pos is None else pos.data_ptr(), pb, pt, int(start))
-
-
-def _qk_shapes(rope, Q, K):
-    if Q.dim() != 4 or (K is not None and K.dim() != 4):
-        raise ValueError("Q and K must be [B, H, n, d]")
-    B, Hq, n, d = Q.shape
-    if d != rope.d:
-        raise ValueError(f"Rope of {rope.d} channels for heads of {d}")
-    Hk = 0 if K is None else K.shape[1]
-    return B, n, Hq, Hk, (B, Hq, n, d), (B, Hk, n, d)
-
-
-def _run_rope(entry, rope, Q, K, pos, start, Qo, Ko, stream):
-    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    dtype, device = Q.dtype, Q.device
-
-    def call(st):
-        yq = _new(Q) if Qo is None else Qo
-        yk = None if K is None else _new(K) if Ko is None else Ko
-        pair = lambda k: None if k is None else _heads("K", k, ks, dtype, device)
-        held, v = _views((_heads("Q", Q, qs, dtype, device), pair(K), _heads("output of Q", yq, qs, dtype, device), pair(yk)))
-        _check(getattr(lib(), entry)(ctypes.byref(rope.c(Q, B, n, pos, start)), B, n, Hq, Hk, *v, st), entry)
-        return yq, yk
-    return _launch(device, stream, call)
+        self.plan = marshal().RopePlan(self.d, self.r, self.interleaved, self.factor, self.turns)
 
 
 def rope_fwd(rope: Rope, Q, K=None, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
     """Rotary positions on Q [B, Hq, n, d] and K [B, Hk, n, d] (or None) in one launch: returns Qr, Kr.  Token t of batch element b
     stands at pos[b, t] (int32 [B, n] or [n]), or at start + t.  Any strides with adjacent channels; Qr = Q, Kr = K work in place."""
-    return _run_rope("rope_fwd", rope, Q, K, pos, start, Qr, Kr, stream)
+    return _on(stream, Q, marshal().rope, False, rope.plan, Q, K, pos, start, Qr, Kr)
 
 
 def rope_bwd(rope: Rope, dQr, dKr=None, pos=None, start: int = 0, dQ=None, dK=None, stream=None):
     """Adjoint of rope_fwd: dQ, dK from the gradients of Qr and Kr (the transposed rotation; Q and K are not needed)."""
-    return _run_rope("rope_bwd", rope, dQr, dKr, pos, start, dQ, dK, stream)
+    return _on(stream, dQr, marshal().rope, True, rope.plan, dQr, dKr, pos, start, dQ, dK)
 
 
 def qk_norm_rope_fwd(rope: Rope, Q, K, gq=None, gk=None, eps: float = 1e-6, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
     """Qr = rope(gq * Q / rms(Q)), Kr = rope(gk * K / rms(K)), rms over the d channels of every head, in one pass.  gq, gk: fp32 [d]
     or None; K may be None; positions, strides and outputs as in rope_fwd."""
-    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    dtype, device = Q.dtype, Q.device
-
-    def call(st):
-        yq = _new(Q) if Qr is None else Qr
-        yk = None if K is None else _new(K) if Kr is None else Kr
-        pair = lambda k: None if k is None else _heads("K", k, ks, dtype, device)
-        held, v = _views((_heads("Q", Q, qs, dtype, device), pair(K), _heads("Qr", yq, qs, dtype, device), pair(yk)))
-        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), device)
-        _check(lib().qk_norm_rope_fwd(ctypes.byref(rope.c(Q, B, n, pos, start)), B, n, Hq, Hk, eps, gain("gq", gq), gain("gk", gk), *v, st),
-               "qk_norm_rope_fwd")
-        return yq, yk
-    return _launch(device, stream, call)
+    return _on(stream, Q, marshal().qk_norm_rope_fwd, rope.plan, Q, K, gq, gk, eps, pos, start, Qr, Kr)
 
 
 def qk_norm_rope_bwd(rope: Rope, Q, K, dQr, dKr, gq=None, gk=None, eps: float = 1e-6, pos=None, start: int = 0, dQ=None, dK=None, stream=None):
     """Adjoint of qk_norm_rope_fwd: dQ, dK, dgq, dgk (fp32 [d]; None where the gain, or K, is None).  Q and K are the inputs of the
     forward call."""
-    B, n, Hq, Hk, qs, ks = _qk_shapes(rope, Q, K)
-    dtype, device = Q.dtype, Q.device
-
-    def call(st):
-        xq = _new(Q) if dQ is None else dQ
-        xk = None if K is None else _new(K) if dK is None else dK
-        pair = lambda name, k: None if k is None else _heads(name, k, ks, dtype, device)
-        held, v = _views((_heads("Q", Q, qs, dtype, device), pair("K", K), _heads("dQr", dQr, qs, dtype, device), pair("dKr", dKr),
-                          _heads("dQ", xq, qs, dtype, device), pair("dK", xk)))
-        gain = lambda name, t: _vector(name, t, torch.float32, (rope.d,), device)
-        dgq, dgk = None if gq is None else _new(gq), None if gk is None or K is None else _new(gk)
-        cr = rope.c(Q, B, n, pos, start)
-        ws = _bytes(lib().qk_norm_rope_bwd_workspace_bytes(ctypes.byref(cr), B, n, Hq, Hk), device)
-        _check(lib().qk_norm_rope_bwd(ctypes.byref(cr), B, n, Hq, Hk, eps, gain("gq", gq), gain("gk", gk), *v, _ptr(dgq), _ptr(dgk),
-                                      ws.data_ptr(), ws.numel(), st), "qk_norm_rope_bwd")
-        return xq, xk, dgq, dgk
-    return _launch(device, stream, call)
+    return _on(stream, Q, marshal().qk_norm_rope_bwd, rope.plan, Q, K, dQr, dKr, gq, gk, eps, pos, start, dQ, dK)
 
 
 # ------------------------------------------------------------------------------------------ softmax attention
-@dataclass
+@dataclass(frozen=True)
 class SoftmaxAttention:
     """Scores and masks of softmax attention of Q [B, Hq, nq, d] on K, V [B, Hk, nk, d] (Hk divides Hq).
 
@@ -706,60 +628,25 @@ class SoftmaxAttention:
     doc_k: Optional[torch.Tensor] = field(default=None, repr=False)
     kv_len: Optional[torch.Tensor] = field(default=None, repr=False)
 
-    def c(self, Q, K) -> _CSoftmax:
-        if Q.dim() != 4 or K.dim() != 4:
-            raise ValueError("Q and K must be [B, H, n, d]")
-        B, Hq, nq, d = Q.shape
-        Hk, nk = K.shape[1], K.shape[2]
-        whole = lambda name, t, s: _vector(name, t, torch.int32, s, Q.device)
-        return _CSoftmax(B, Hq, Hk, nq, nk, d, _dtype_code(Q), 1.0 / math.sqrt(d) if self.scale is None else float(self.scale),
-                         float(self.cap), int(bool(self.causal)), whole("prefix", self.prefix, (B,)), whole("kv_len", self.kv_len, (B,)),
-                         _vector("slopes", self.slopes, torch.float32, (Hq,), Q.device), whole("doc_q", self.doc_q, (B, nq)),
-                         whole("doc_k", self.doc_k, (B, nk)))
+    def __post_init__(self):
+        plan = marshal().SmPlan(self.scale, self.cap, self.causal, self.prefix, self.slopes, self.doc_q, self.doc_k, self.kv_len)
+        object.__setattr__(self, "plan", plan)
 
 
 def softmax_attention_workspace_bytes(sp: SoftmaxAttention, Q, K, backward: bool) -> int:
-    cs = sp.c(Q, K)
-    return int(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), int(backward)))
+    return marshal().softmax_bytes(sp.plan, Q, K, backward)
 
 
 def softmax_attention_fwd(sp: SoftmaxAttention, Q, K, V, O=None, lse=None, ws=None, dev_status=None, stream=None):
     """O [B, Hq, nq, d] and lse fp32 [B, Hq, nq] (the logarithm of every row's sum; both are what the backward pass wants).  A row
     that the masks leave empty gets O = 0, lse = -inf.  Any strides with adjacent channels.  ``ws``: a uint8 tensor of
     softmax_attention_workspace_bytes(...), or None; calls that may overlap need one each."""
-    cs = sp.c(Q, K)
-    qs, ks = Q.shape, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    dtype, device = Q.dtype, Q.device
-
-    def call(st):
-        out = _new(Q) if O is None else O
-        sums = torch.empty(qs[:3], dtype=torch.float32, device=device) if lse is None else lse
-        work = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 0), device) if ws is None else ws
-        held, v = _views((_heads("Q", Q, qs, dtype, device), _heads("K", K, ks, dtype, device), _heads("V", V, ks, dtype, device),
-                          _heads("O", out, qs, dtype, device)))
-        _check(lib().softmax_attention_fwd(ctypes.byref(cs), *v, _vector("lse", sums, torch.float32, qs[:3], device), _ptr(work), work.numel(),
-                                           _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), device), st), "softmax_attention_fwd")
-        return out, sums
-    return _launch(device, stream, call)
+    return _on(stream, Q, marshal().softmax_fwd, sp.plan, Q, K, V, O, lse, ws, dev_status)
 
 
 def softmax_attention_bwd(sp: SoftmaxAttention, Q, K, V, O, lse, dO, dQ=None, dK=None, dV=None, ws=None, dev_status=None, stream=None):
     """Adjoint of softmax_attention_fwd: dQ, dK, dV.  O and lse are the forward call's."""
-    cs = sp.c(Q, K)
-    qs, ks = Q.shape, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    dtype, device = Q.dtype, Q.device
-
-    def call(st):
-        gq, gk, gv = _new(Q) if dQ is None else dQ, _new(Q, ks) if dK is None else dK, _new(Q, ks) if dV is None else dV
-        work = _bytes(lib().softmax_attention_workspace_bytes(ctypes.byref(cs), 1), device) if ws is None else ws
-        one = lambda name, t, s: _heads(name, t, s, dtype, device)
-        held, v = _views((one("Q", Q, qs), one("K", K, ks), one("V", V, ks), one("O", O, qs), one("dO", dO, qs), one("dQ", gq, qs), one("dK", gk, ks),
-                          one("dV", gv, ks)))
-        _check(lib().softmax_attention_bwd(ctypes.byref(cs), *v[:4], _vector("lse", lse, torch.float32, qs[:3], device), *v[4:], _ptr(work),
-                                           work.numel(), _vector("dev_status", dev_status, torch.int32, (qs[0] * qs[1],), device), st),
-               "softmax_attention_bwd")
-        return gq, gk, gv
-    return _launch(device, stream, call)
+    return _on(stream, Q, marshal().softmax_bwd, sp.plan, Q, K, V, O, lse, dO, dQ, dK, dV, ws, dev_status)
 
 
 # ------------------------------------------------------------------------------------------ profiling aid

@@ -4,13 +4,16 @@ from __future__ import annotations
 import glob
 import os
 import re
+import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "liblaplace_nystrom.so")
 OBJ_DIR = os.path.join(LIB_DIR, "obj")
+MARSHAL = os.path.join(LIB_DIR, "_ln_torch.so")      # argument marshalling for torch tensors, a Python module
 ROOT = os.path.dirname(HERE)
 
 NVCC_FLAGS = [
@@ -69,5 +72,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_marshal(force: bool = False) -> str:
+    """Compile csrc/ln_torch.cpp against torch's headers into lib/_ln_torch.so if it or a file it includes changed."""
+    import torch
+    src = os.path.join(CSRC, "ln_torch.cpp")
+    header = os.path.join(ROOT, "include", "laplace_nystrom.h")
+    if not force and os.path.exists(MARSHAL) and _newest([src, header]) <= os.path.getmtime(MARSHAL):
+        return MARSHAL
+    os.makedirs(LIB_DIR, exist_ok=True)
+    torch_dir = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(ROOT, "include"), os.path.join(torch_dir, "include"),
+               os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+               os.path.join(cuda, "include")]
+    lib = os.path.join(torch_dir, "lib")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_EXTENSION_NAME=_ln_torch",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+                          + [f for d in include for f in ("-isystem" if d != include[0] else "-I", d)]
+                          + [src, "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
+    print(build_marshal(force=True))
