@@ -284,9 +284,9 @@ template <int D> int softmax_bwd_umma(const SmArgs& a, cudaStream_t st) {
       !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 64, &mk) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 64, &mv)) return LN_ERR_CUDA;
   auto go = [&](auto q, auto kv) {
     want_smem(q, SuBwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_bwd_q", st, enqueue(q, dim3(a.B * a.Hq, cdiv(a.nq, 128)), SU_THREADS, SuBwd<D>::kSmem, st, a, sq, sdo, mk, mv));
+    LN_LAUNCH("k_softmax_bwd_q", st, enqueue(q, dim3(a.B * a.Hq, cdiv(a.nq, 128)), SuBwd<D>::kThreads, SuBwd<D>::kSmem, st, a, sq, sdo, mk, mv));
     want_smem(kv, SuBwd<D>::kSmem);
-    LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(a.B * a.Hk, cdiv(a.nk, 128)), SU_THREADS, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
+    LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(a.B * a.Hk, cdiv(a.nk, 128)), SuBwd<D>::kThreads, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
   };
   if (a.cap > 0.f) {
     if (a.slopes) go(k_softmax_bwd_umma<D, true, true, false>, k_softmax_bwd_umma<D, true, true, true>);

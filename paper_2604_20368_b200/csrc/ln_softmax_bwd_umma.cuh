@@ -1,13 +1,18 @@
 // Softmax attention on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 storage, backward.
 //
 // One CTA = 128 stationary rows X of one head; the moving rows Y stream through shared memory in tiles of 64, copied by TMA.
-//   queries stationary (KEYS false):  X1 = Q, X2 = dO;  Y1 = K, Y2 = V;   dQ += ds Y1
+//   queries stationary (KEYS false):  X1 = Q, X2 = dO;  Y1 = K, Y2 = V;   dQ += ds Y1, M += A Y1
 //   keys stationary    (KEYS true):   X1 = K, X2 = V;   Y1 = Q, Y2 = dO of every query head of the group;  dK += ds Y1, dV += A Y2
 // Per tile: S = X1 Y1^T and dP = X2 Y2^T (128 x 64, K = d, operands in shared memory), then A = exp2(x - lse) and
 // ds = A (dP - delta) (1 - tanh^2), both rounded to bf16 and written over S and dP in TMEM, from where they are the left operands
-// of the products into the accumulators (128 x d in TMEM).  S and dP are double-buffered: warps 0-3 form the exponentials of the
-// even tiles, warps 4-7 those of the odd ones (a thread owns a row), and while one group waits for the tensor core the other has
-// work.  Warp 8 copies, warp 9 issues the products.  `scale` is applied once, to the accumulators.
+// of the products into the accumulators (128 x d in TMEM).  A thread owns a row of a group of four warps.  With 128 channels S and dP
+// have two buffers (NB = 2): one group forms the exponentials of the even tiles, one those of the odd ones, and while one waits for
+// the tensor core the other has work.  With 64 channels a CTA has one buffer and one group, and two CTAs share an SM, which
+// hides the start and the end of a CTA too.  One warp copies, one issues the products.  `scale` is applied once, to the accumulators.
+// delta from the stored O is off by O's rounding, up to 2^-8 sum|dO||O|, more than anything else where a row's softmax is
+// peaked.  The sum of a row's ds says by how much (it is zero for the right delta): the query pass adds it up in 32 bits, takes it
+// times M = A K off dQ, and hands the corrected delta to the key pass (dQ and dK of 4096 tokens with scores of 3 standard deviations:
+// 2.7e-3 -> 2.4e-3 of their norm, of 16 tokens 4.0e-3 -> 2.4e-3, where their own rounding is 1.7e-3).
 // Two passes form S and dP twice (7 products a pair instead of 5): no atomics, and every sum has one order.
 // Bound by the tensor core's operand reads: with 64 columns a product reads 128 + 64 rows of shared memory for 128 x 64 results.
 #pragma once
@@ -15,26 +20,26 @@
 
 namespace ln {
 
-constexpr int SU_THREADS = 320;
 template <int D> struct SuBwd {
   static constexpr int kX = 128 * D * 2, kY = 64 * D * 2;         // bytes of a stationary and of a moving tile
-  static constexpr int kStages = 4;
+  static constexpr int kBuffers = D == 64 ? 1 : 2, kStages = D == 64 ? 3 : 4;
+  static constexpr int kThreads = kBuffers * 128 + 64, kCtas = D == 64 ? 2 : 1, kTmem = D == 64 ? 256 : 512;
   static constexpr size_t kSmem = 1024 + 2 * (size_t)kX + 2 * (size_t)kY * kStages;
 };
 
 template <int D, bool CAP, bool BIAS, bool KEYS>
-__global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mx1,
-                                                                  const __grid_constant__ TileMap mx2, const __grid_constant__ TileMap my1,
-                                                                  const __grid_constant__ TileMap my2) {
+__global__ void __launch_bounds__(SuBwd<D>::kThreads, SuBwd<D>::kCtas)
+k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mx1, const __grid_constant__ TileMap mx2,
+                   const __grid_constant__ TileMap my1, const __grid_constant__ TileMap my2) {
   pdl_wait();
-  constexpr int NS = SuBwd<D>::kStages, XB = SuBwd<D>::kX, YB = SuBwd<D>::kY;
+  constexpr int NS = SuBwd<D>::kStages, XB = SuBwd<D>::kX, YB = SuBwd<D>::kY, NB = SuBwd<D>::kBuffers, COPY = 4 * NB, MMA = 4 * NB + 1;
   extern __shared__ __align__(16) char su_smem[];
   char* base = su_smem + ((1024u - (umma::s32(su_smem) & 1023u)) & 1023u);
   char *sX = base, *sY = base + 2 * XB;                                      // X1, X2; per stage Y1, Y2
-  __shared__ unsigned long long x_full, y_full[NS], y_free[NS], y_raw, l_full[NS], s_full[2], p_ready[2], acc_full, spare;
+  __shared__ unsigned long long x_full, y_full[NS], y_free[NS], y_raw, l_full[NS], s_full[NB], p_ready[NB], acc_full, spare;
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float sL[KEYS ? NS : 1][64], sD[KEYS ? NS : 1][64];     // -lse (base 2) and -delta of the moving queries
-  __shared__ float sDelta[KEYS ? 1 : 2][128];
+  __shared__ float sRow[KEYS ? 1 : NB][128];                                 // a group's part of a row's delta, then of its sum of ds
   __shared__ int sh[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int H = KEYS ? a.Hk : a.Hq, b = blockIdx.x / H, hs = blockIdx.x % H;
@@ -45,20 +50,20 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   if (tid == 0) {
     umma::mbar_init(&x_full, 1); umma::mbar_init(&y_raw, 1); umma::mbar_init(&acc_full, 1); umma::mbar_init(&spare, 1);
     for (int s = 0; s < NS; ++s) { umma::mbar_init(&y_full[s], 1); umma::mbar_init(&y_free[s], 1); umma::mbar_init(&l_full[s], 1); }
-    for (int t = 0; t < 2; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); }
+    for (int t = 0; t < NB; ++t) { umma::mbar_init(&s_full[t], 1); umma::mbar_init(&p_ready[t], 4); }
   }
-  if (warp == 9) umma::tmem_alloc(&tmem_slot, 512);
+  if (warp == MMA) umma::tmem_alloc(&tmem_slot, SuBwd<D>::kTmem);
   umma::fence_before_sync();
   __syncthreads();
   umma::fence_after_sync();
-  const uint32_t tm = tmem_slot;                                             // S, dP of buffer 0, of buffer 1 (64 columns each); accumulators
-  constexpr int ACC2 = 256, ACC1 = 256 + D;                                  // ds Y1;  A Y2
+  const uint32_t tm = tmem_slot;                                             // S, dP (64 columns each) of every buffer; accumulators
+  constexpr int ACC2 = NB * 128, ACC1 = NB * 128 + D;                        // ds Y1;  A Y2 (keys stationary) or A Y1
   const int* dq = a.doc_q ? a.doc_q + (long long)b * a.nq : nullptr;
   const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
   const int first_head = KEYS ? hs * a.group : hs;                           // query head of the first moving tile
   bool ok = true;
 
-  if (warp == 8) {                                                           // copies
+  if (warp == COPY) {                                                           // copies
     const bool one = umma::elect_one();
     if (total > 0 && one) {
       umma::mbar_expect_tx(&x_full, 2 * XB);
@@ -112,13 +117,13 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
     if (!ok)                                                                 // no copy is in flight when the CTA ends
       for (int s = 0; s < NS; ++s)
         if (n > s) umma::mbar_wait(&y_full[s], (uint32_t)((n - 1 - s) / NS) & 1);
-  } else if (warp == 9) {                                                    // products
+  } else if (warp == MMA) {                                                    // products
     if (umma::elect_one() && total > 0) {
       const uint32_t id_s = umma::instr_desc(64, false, false), id_a = umma::instr_desc(D, false, true);
       const uint64_t x1 = umma::rows_desc(umma::s32(sX)), x2 = x1 + (XB >> 4), yr = umma::rows_desc(umma::s32(sY)), yc = umma::cols_desc(umma::s32(sY), 64);
       auto arrived = [&](int n) { ok = ok && umma::mbar_wait(&y_full[n % NS], (uint32_t)(n / NS) & 1); };
       auto scores = [&](int n) {                                             // S and dP of tile n (d = 32: the upper channels are zeros)
-        const int s = n % NS, buf = n & 1;
+        const int s = n % NS, buf = n % NB;
         const uint64_t y1 = yr + (uint64_t)(s * (2 * YB >> 4)), y2 = y1 + (YB >> 4);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) umma::mma(tm + buf * 128, x1 + umma::rows_step(128, ks), y1 + umma::rows_step(64, ks), id_s, ks > 0);
@@ -130,33 +135,33 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
       arrived(0);
       umma::fence_after_sync();
       if (ok) scores(0);
-      if (total > 1) {
+      if (NB > 1 && total > 1) {
         arrived(1);
         if (ok) scores(1);
       }
       for (int n = 0; n < total && ok; ++n) {
-        const int s = n % NS, buf = n & 1;
+        const int s = n % NS, buf = n % NB;
         const uint64_t y1 = yc + (uint64_t)(s * (2 * YB >> 4)), y2 = y1 + (YB >> 4);
-        // a wait costs some 200 clocks beside the products' operand reads, so the one for tile n + 2 comes while this tile's
+        // a wait costs some 200 clocks beside the products' operand reads, so the one for tile n + NB comes while this tile's
         // exponentials are still being formed
-        if (n + 2 < total) arrived(n + 2);
-        ok = ok && umma::mbar_wait(&p_ready[buf], (uint32_t)(n >> 1) & 1);
+        if (n + NB < total) arrived(n + NB);
+        ok = ok && umma::mbar_wait(&p_ready[buf], (uint32_t)(n / NB) & 1);
         if (!ok) break;
         umma::fence_after_sync();
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {                                     // 64 columns became 32 packed ones at the front of their place
           const uint32_t at = tm + buf * 128 + ks * 8;
-          if (KEYS) umma::mma_ta(tm + ACC1, at, y2 + umma::cols_step(ks), id_a, n > 0 || ks > 0);
+          umma::mma_ta(tm + ACC1, at, (KEYS ? y2 : y1) + umma::cols_step(ks), id_a, n > 0 || ks > 0);
           umma::mma_ta(tm + ACC2, at + 64, y1 + umma::cols_step(ks), id_a, n > 0 || ks > 0);
         }
         if (n + NS < total) umma::commit(&y_free[s]);                        // only where the copying warp waits for it
-        if (n + 2 < total) scores(n + 2);
+        if (n + NB < total) scores(n + NB);
       }
       if (ok) umma::commit(&acc_full);
       else { umma::commit(&spare); umma::mbar_wait(&spare, 0); }             // no product is in flight when the CTA ends
     }
   } else {                                                                   // exponentials
-    const int half = warp >> 2, row = (warp & 3) * 32 + lane, r = s0 + row;
+    const int group = warp >> 2, row = (warp & 3) * 32 + lane, r = s0 + row;
     const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
     int doc, lo, hi;                                                         // moving tokens [lo, hi) are left by the masks but the documents'
     float rowL = 0.f, rowD = 0.f;
@@ -166,38 +171,48 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
     } else {
       doc = dq && r < a.nq ? dq[r] : 0;
       lo = 0; hi = r < a.nq && doc >= 0 ? m.limit(r) : 0;
-      // delta: two threads a row, half the channels each
+      // delta: a thread of every group a row, its share of the channels each
       const long long at = (long long)blockIdx.x * a.nq + r;
       float v = 0.f;
       if (r < a.nq) {
-        const bf16* o = static_cast<const bf16*>(a.o.p) + b * a.o.b + hs * a.o.h + r * a.o.t + half * (a.d / 2);
-        const bf16* g = static_cast<const bf16*>(a.dout.p) + b * a.dout.b + hs * a.dout.h + r * a.dout.t + half * (a.d / 2);
-        for (int c = 0; c < a.d / 2; c += 4) {
-          const float4 x = ld4(o + c), y = ld4(g + c);
-          v += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
+        const bf16* o = static_cast<const bf16*>(a.o.p) + b * a.o.b + hs * a.o.h + r * a.o.t + group * (a.d / NB);
+        const bf16* g = static_cast<const bf16*>(a.dout.p) + b * a.dout.b + hs * a.dout.h + r * a.dout.t + group * (a.d / NB);
+#pragma unroll 4
+        for (int c = 0; c < a.d / NB; c += 8) {
+          const uint4 x = *reinterpret_cast<const uint4*>(o + c), y = *reinterpret_cast<const uint4*>(g + c);
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), v);
+            v = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), v);
+          }
         }
         rowL = a.lse[at] * kLog2e;
       }
-      sDelta[half][row] = v;
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      rowD = sDelta[0][row] + sDelta[1][row];
-      if (half == 0 && r < a.nq) a.delta[at] = rowD;
+      rowD = v;
+      if (NB > 1) {
+        sRow[group][row] = v;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        rowD = sRow[0][row] + sRow[NB - 1][row];
+        asm volatile("bar.sync 1, 256;" ::: "memory");                       // read by both before it takes the sums of ds
+      }
     }
+    f32x2 rest2 = pack2(0.f, 0.f);                                           // sum of this row's ds before the cap's factor
     const int* dm = KEYS ? dq : dk;
-    const int nm = KEYS ? a.nq : a.nk, buf = half;
+    const int nm = KEYS ? a.nq : a.nk, buf = group;
     SmScore sc = sm_score_of(a, first_head);
     const f32x2 ka = pack2(CAP ? -2.f * sc.cap2 : sc.mul, CAP ? -2.f * sc.cap2 : sc.mul), kb = pack2(sc.cap2, sc.cap2);
     const f32x2 rowL2 = pack2(-rowL, -rowL), rowD2 = pack2(-rowD, -rowD);
     const uint32_t ts = tm + quarter + buf * 128;
-    int tile = range.x + half, head = first_head;                            // of moving tile n
+    int tile = range.x + group, head = first_head;                            // of moving tile n
     uint32_t turn = 0;                                                       // how often this group has waited for its buffer
-    for (int n = half; n < total; n += 2, ++turn) {
+    for (int n = group; n < total; n += NB, ++turn) {
       while (tile >= range.x + nt) {                                         // the next query head of the group
         tile -= nt; ++head;
         if (BIAS) sc.slope2 = a.slopes[head] * kLog2e;
       }
       const int s = n % NS, m0 = tile * 64;
-      tile += 2;
+      tile += NB;
       const bool whole = KEYS ? s0 + 128 <= a.nk && sm_whole(a, m, b, m0, m0 + 64, s0, s0 + 128) : sm_whole(a, m, b, s0, s0 + 128, m0, m0 + 64);
       ok = (!KEYS || warp_wait(&l_full[s], (uint32_t)(n / NS) & 1)) && warp_wait(&s_full[buf], turn & 1);
       if (!ok) break;
@@ -245,17 +260,26 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             f32x2 v = mul2(pack2(p[2 * k], p[2 * k + 1]), add2(pack2(g[e + 2 * k], g[e + 2 * k + 1]), Dl[k]));
-            if (CAP) v = mul2(v, bend[k]);
             unpack2(v, d[2 * k], d[2 * k + 1]);
           }
           if (MASKED)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               if (!((left >> (e + k)) & 1u)) d[k] = 0.f;
-          if (KEYS) { wp[e / 2] = umma::pack_bf16(p[0], p[1]); wp[e / 2 + 1] = umma::pack_bf16(p[2], p[3]); }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            f32x2 v = pack2(d[2 * k], d[2 * k + 1]);
+            if (!KEYS) rest2 = add2(rest2, v);
+            if (CAP) {
+              v = mul2(v, bend[k]);
+              unpack2(v, d[2 * k], d[2 * k + 1]);
+              if (!KEYS) unpack2(mul2(pack2(p[2 * k], p[2 * k + 1]), bend[k]), p[2 * k], p[2 * k + 1]);
+            }
+          }
+          { wp[e / 2] = umma::pack_bf16(p[0], p[1]); wp[e / 2 + 1] = umma::pack_bf16(p[2], p[3]); }
           wd[e / 2] = umma::pack_bf16(d[0], d[1]); wd[e / 2 + 1] = umma::pack_bf16(d[2], d[3]);
         }
-        if (KEYS) umma::tmem_st16(ts + c0 / 2, wp);
+        umma::tmem_st16(ts + c0 / 2, wp);
         umma::tmem_st16(ts + 64 + c0 / 2, wd);
       };
       if (whole) {
@@ -274,38 +298,56 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
       ok = ok && warp_wait(&acc_full, 0);
       umma::fence_after_sync();
     }
+    float rest = 0.f;
+    if (!KEYS) {
+      float u;
+      unpack2(rest2, rest, u);
+      rest += u;
+      if (NB > 1) {
+        sRow[group][row] = rest;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        rest = sRow[0][row] + sRow[NB - 1][row];
+      }
+      if (group == 0 && r < a.nq) a.delta[(long long)blockIdx.x * a.nq + r] = rowD + rest;
+    }
     if (ok) {
-      // rows of this warp, its half of the channels, through its part of the stationary tiles (no product reads them any more)
-      constexpr int HC = D / 2, PR = HC / 8;
-      const int rows = (KEYS ? a.nk : a.nq) - s0 - (warp & 3) * 32, pieces = min(max(a.d - half * HC, 0), HC) / 8;
+      // rows of this warp, its group's share of the channels, through its part of the stationary tiles (no product reads them any more)
+      constexpr int HC = D / NB, PR = HC / 8;
+      const int rows = (KEYS ? a.nk : a.nq) - s0 - (warp & 3) * 32, pieces = min(max(a.d - group * HC, 0), HC) / 8;
 #pragma unroll
       for (int out = 0; out < (KEYS ? 2 : 1); ++out) {
         char* stage = sX + out * XB + (warp * 32 * HC) * 2;
         const float mul = out ? 1.f : a.scale;
 #pragma unroll
         for (int c = 0; c < HC; c += 32) {
-          float o[32];
+          float o[32], w1[32];
           if (total > 0) {
-            umma::tmem_ld32_async(tm + quarter + (out ? ACC1 : ACC2) + half * HC + c, o);
+            umma::tmem_ld32_async(tm + quarter + (out ? ACC1 : ACC2) + group * HC + c, o);
+            if (!KEYS) umma::tmem_ld32_async(tm + quarter + ACC1 + group * HC + c, w1);
             umma::tmem_ld_wait();
             umma::tie32(o);
+            if (!KEYS) {
+              umma::tie32(w1);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = fmaf(-rest, w1[e], o[e]);
+            }
           }
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = total > 0 ? umma::pack_bf16(o[8 * q + 2 * e] * mul, o[8 * q + 2 * e + 1] * mul) : 0u;
-            *reinterpret_cast<uint4*>(stage + (lane * PR + ((c / 8 + q) ^ (lane & (PR - 1)))) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(stage + (lane * PR + ((c / 8 + q) ^ (lane & 7))) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
         __syncwarp();
         const SmView& v = out ? a.dv : (KEYS ? a.dk : a.dq);
-        bf16* G = static_cast<bf16*>(v.p) + b * v.b + hs * v.h + half * HC;
+        bf16* G = static_cast<bf16*>(v.p) + b * v.b + hs * v.h + group * HC;
         const long long first = s0 + (warp & 3) * 32;
         for (int e = lane; e < 32 * pieces; e += 32) {
           const int rr = e / pieces, p = e % pieces;
           if (rr < rows)
-            *reinterpret_cast<uint4*>(G + (first + rr) * v.t + p * 8) = *reinterpret_cast<const uint4*>(stage + (rr * PR + (p ^ (rr & (PR - 1)))) * 16);
+            *reinterpret_cast<uint4*>(G + (first + rr) * v.t + p * 8) = *reinterpret_cast<const uint4*>(stage + (rr * PR + (p ^ (rr & 7))) * 16);
         }
       }
     }
@@ -313,7 +355,7 @@ __global__ void __launch_bounds__(SU_THREADS, 1) k_softmax_bwd_umma(const __grid
   __syncwarp();
   umma::fence_before_sync();
   __syncthreads();
-  if (warp == 9) umma::tmem_dealloc(tm, 512);
+  if (warp == MMA) umma::tmem_dealloc(tm, SuBwd<D>::kTmem);
   umma::report_timeout(ok, a.dev_status, KEYS ? b * a.Hq + first_head : (int)blockIdx.x);
 }
 

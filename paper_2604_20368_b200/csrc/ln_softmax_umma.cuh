@@ -69,16 +69,22 @@ template <int D, typename F> __device__ __forceinline__ void tile_clear(char* ti
 // A bounded wait whose outcome is the same in every lane.
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, umma::mbar_wait(bar, parity)); }
 
-// The 32 moving tokens from j that the masks leave a row, as bits: [from, to), and those of its document.
+// The 32 moving tokens from j that the masks leave a row, as bits: [from, to), and those of its document.  A whole warp, a row a lane:
+// a lane fetches one token's document, and a turn of the loop serves all the tokens and rows of one document.
 __device__ __forceinline__ uint32_t sm_left(int from, int to, const int* dm, int doc, int j, int n) {
   from = max(from - j, 0); to = min(max(to - j, 0), 32);
   uint32_t left = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & (from < 32 ? 0xffffffffu << from : 0u);
-  if (dm)
-#pragma unroll 8
-    for (int e = 0; e < 32; ++e) {
-      const int id = j + e < n ? __ldg(dm + j + e) : -1;          // the same address for the whole warp
-      if (id != doc) left &= ~(1u << e);
+  if (dm) {
+    const int at = j + (int)(threadIdx.x & 31), id = at < n ? dm[at] : -1;
+    uint32_t todo = 0xffffffffu, mine = 0;
+    while (todo) {
+      const int d = __shfl_sync(0xffffffffu, id, __ffs(todo) - 1);
+      const uint32_t same = __ballot_sync(0xffffffffu, id == d);
+      if (doc == d) mine = same;
+      todo &= ~same;
     }
+    left &= mine;
+  }
   return left;
 }
 
