@@ -123,11 +123,11 @@ int check_softmax(const ln_softmax* p, bool bwd) {
   return LN_OK;
 }
 
-// A serving step: the rows that share a key head fit one 16-row tile.  Its keys are split over CTAs, four for every SM in all and
-// 256 keys at least.
+// A serving step: the rows that share a key head fit one 16-row tile.  Its keys are split over CTAs, eight for every SM in all (two are
+// resident; sequences of a batch have different lengths; four or six: a tenth slower, twelve: more to join) and 256 keys at least.
 bool is_step(const ln_softmax* p) { return (long long)(p->Hq / p->Hk) * p->nq <= ST_ROWS; }
 StepPlan plan_step(const ln_softmax* p) {
-  const long long heads = (long long)p->B * p->Hk, want = (4ll * sm_count() + heads - 1) / heads;
+  const long long heads = (long long)p->B * p->Hk, want = (8ll * sm_count() + heads - 1) / heads;
   long long chunk = (p->nk + want - 1) / want;
   chunk = (chunk + 127) / 128 * 128;
   if (chunk < 256) chunk = 256;
@@ -207,19 +207,24 @@ void softmax_docs(const SmArgs& a, const SmWork& w, cudaStream_t st) {
 }
 
 template <typename T> void softmax_join(const SmArgs& a, int splits, const StepPart& part, cudaStream_t st) {
-  LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<T>, dim3(cdiv((long long)a.B * a.Hq * a.nq, 4)), 128, 0, st, a, StepPlan{0, splits}, part));
+  const long long rows = (long long)a.B * a.Hq * a.nq;
+  if (rows <= 16ll * sm_count()) LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<T, 4>, dim3((unsigned)rows), 128, 0, st, a, splits, part));
+  else LN_LAUNCH("k_softmax_join", st, enqueue(k_softmax_join<T, 1>, dim3(cdiv(rows, 4)), 128, 0, st, a, splits, part));
 }
 
 void softmax_step(const ln_softmax* p, const SmArgs& a, const SmWork& w, cudaStream_t st) {
   const StepPlan s = plan_step(p);
   const dim3 grid(s.splits, a.B * a.Hk);
-  auto go = [&](auto kern) { LN_LAUNCH("k_softmax_step", st, enqueue(kern, grid, ST_WARPS * 32, 0, st, a, s, w.part)); };
+  auto go = [&](auto kern, size_t smem = 0) {
+    if (smem) want_smem(kern, smem);
+    LN_LAUNCH("k_softmax_step", st, enqueue(kern, grid, ST_WARPS * 32, smem, st, a, s, w.part));
+  };
   auto f32 = [&](auto d) {
     constexpr int D = decltype(d)::value;
     const int rows = a.group * a.nq;
     if (rows == 1) go(k_softmax_step_f32<D, 1>); else if (rows <= 4) go(k_softmax_step_f32<D, 4>); else go(k_softmax_step_f32<D, ST_ROWS>);
   };
-  if (p->dtype == LN_BF16) { if (p->d == 32) go(k_softmax_step<32>); else if (p->d == 64) go(k_softmax_step<64>); else go(k_softmax_step<128>); }
+  if (p->dtype == LN_BF16) { if (p->d == 32) go(k_softmax_step<32>, step_smem<32>()); else if (p->d == 64) go(k_softmax_step<64>, step_smem<64>()); else go(k_softmax_step<128>, step_smem<128>()); }
   else if (p->d == 32) f32(std::integral_constant<int, 32>());
   else if (p->d == 64) f32(std::integral_constant<int, 64>());
   else f32(std::integral_constant<int, 128>());
