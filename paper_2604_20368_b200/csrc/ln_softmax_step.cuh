@@ -114,15 +114,15 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
   extern __shared__ __align__(16) char st_smem[];
   constexpr int NP = step_pieces<D>();
   char* mine = st_smem + (size_t)warp * ST_STAGES * NP * 512 + lane * 16;    // [stage][piece][lane]
-  // the 16 keys from j0: lane group g has keys j0 + g and j0 + 8 + g, and values of j0 + 2 c, + 1, + 8, + 9 (absent ones are zeros
-  // whatever they hold)
+  // the 16 keys from j0: lane group g has keys j0 + g and j0 + 8 + g, and values of j0 + 2 c, + 1, + 8, + 9.  Absent ones are zeros
+  // whatever they hold: a value is multiplied by its zero, and a cap's reciprocal is shared by four scores.
   auto fetch = [&](int j0, int stage) {
     char* to = mine + stage * NP * 512;
     if (j0 < k1) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int j = j0 + 8 * t + g;
-        const bool in = j < k1;
+        const bool in = j < k1 && !(dk && dk[j] < 0);
         const bf16* row = K + (in ? (long long)j * a.k.t : 0) + c * 8;
 #pragma unroll
         for (int l = 0; l < KL; ++l) step_copy<16>(to + (t * KL + l) * 512, row + l * 32, in);

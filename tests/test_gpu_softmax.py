@@ -150,6 +150,25 @@ def test_steps_over_a_long_cache(dtype, d, Hq, Hk, nq):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("nq", [1, 3, 30])
+@pytest.mark.parametrize("cap", [0.0, 10.0])
+def test_padding_between_the_keys_of_a_step_may_hold_anything(dtype, nq, cap):
+    nk = 600
+    g = torch.Generator().manual_seed(7)
+    Q, K, V, dO = _inputs(2, 4, 2, nq, nk, 64, dtype)
+    dk = torch.randint(-1, 2, (2, nk), generator=g).int()
+    dq = torch.randint(0, 2, (2, nq), generator=g).int()
+    kw = dict(doc_q=dq, doc_k=dk, cap=cap, slopes=_slopes(4))
+    got = _compare(Q, K, V, dO, **kw)
+    pad = (dk < 0).to(DEV)
+    K.transpose(1, 2)[pad] = float("nan")
+    V.transpose(1, 2)[pad] = float("inf")
+    again = _run(Q, K, V, dO, **kw)
+    for k in got:
+        assert torch.equal(got[k], again[k]), k
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
 def test_long_row_and_large_scores(dtype):
     # scores of +-100 and more: the running maximum moves, the exponentials span the whole range
     Q, K, V, dO = _inputs(1, 2, 2, 130, 2100, 64, dtype, sigma=30.0)
