@@ -1,4 +1,4 @@
-"""Thin ctypes binding of ``include/laplace_nystrom.h``.
+"""Thin binding of ``include/laplace_nystrom.h``: ctypes, and for the operators of a serving step a module in C++.
 
 Argument marshalling only: every step of the path runs in the CUDA library.  torch is used
 for device memory and streams.  There is no CPU fallback: if the shared library cannot be

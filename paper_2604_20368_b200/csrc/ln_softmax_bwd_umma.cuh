@@ -15,6 +15,7 @@
 // 2.7e-3 -> 2.4e-3 of their norm, of 16 tokens 4.0e-3 -> 2.4e-3, where their own rounding is 1.7e-3).
 // Two passes form S and dP twice (7 products a pair instead of 5): no atomics, and every sum has one order.
 // Bound by the tensor core's operand reads: with 64 columns a product reads 128 + 64 rows of shared memory for 128 x 64 results.
+// 32 heads of 4096 tokens without masks: 128 channels query pass 486 us, key pass 458 (1.20 PFLOP/s); 64 channels 310 and 345.
 #pragma once
 #include "ln_softmax_umma.cuh"
 
