@@ -611,7 +611,7 @@ def qk_norm_rope_bwd(rope: Rope, Q, K, dQr, dKr, gq=None, gk=None, eps: float = 
 
 
 # ------------------------------------------------------------------------------------------ softmax attention
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class SoftmaxAttention:
     """Scores and masks of softmax attention of Q [B, Hq, nq, d] on K, V [B, Hk, nk, d] (Hk divides Hq).
 

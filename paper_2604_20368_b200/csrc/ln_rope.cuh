@@ -116,11 +116,11 @@ __global__ void __launch_bounds__(256, MODE == QK_NORM_BWD ? 2 : 4) k_qk_rope(co
     const int b = live ? f / a.n : 0, tok = live ? f % a.n : 0;
     float co[INTER ? E / 2 : E], si[INTER ? E / 2 : E];
     {
-      const int p = a.pos ? a.pos[b * a.pos_b + tok * a.pos_n] : a.start + tok;
+      const long long p = a.pos ? a.pos[b * a.pos_b + tok * a.pos_n] : (long long)a.start + tok;
       if (turned)
 #pragma unroll
         for (int e = 0; e < (INTER ? E / 2 : E); ++e) {
-          turn_sincos((uint32_t)(((unsigned long long)(long long)p * __ldg(turns + e)) >> 32), si[e], co[e]);
+          turn_sincos((uint32_t)(((unsigned long long)p * __ldg(turns + e)) >> 32), si[e], co[e]);
           co[e] *= a.factor;
           si[e] *= a.factor * (INTER ? a.sign : psign);
         }

@@ -25,29 +25,40 @@ __device__ __forceinline__ void sm_tile(float* dst, const T* src, long long stri
   }
 }
 
-// s[k][q] += sum_c A[4 ty + k][c] B[tx + 16 q][c]
+// s[k][q] = sum_c A[4 ty + k][c] B[tx + 16 q][c]; even and odd channels in the halves of a packed multiply-add, which takes one
+// issue slot for both
 template <int D>
 __device__ __forceinline__ void sm_dots(const float* A, const float* B, int ty, int tx, float (&s)[4][4]) {
+  f32x2 p[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) p[k][q] = pack2(0.f, 0.f);
 #pragma unroll 4
   for (int c = 0; c < D; c += 4) {
-    float4 a[4], b[4];
+    ulonglong2 a[4], b[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = *reinterpret_cast<const float4*>(A + (ty * 4 + k) * (D + 4) + c);
+    for (int k = 0; k < 4; ++k) a[k] = *reinterpret_cast<const ulonglong2*>(A + (ty * 4 + k) * (D + 4) + c);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) b[q] = *reinterpret_cast<const float4*>(B + (tx + 16 * q) * (D + 4) + c);
+    for (int q = 0; q < 4; ++q) b[q] = *reinterpret_cast<const ulonglong2*>(B + (tx + 16 * q) * (D + 4) + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        s[k][q] = fmaf(a[k].x, b[q].x, s[k][q]); s[k][q] = fmaf(a[k].y, b[q].y, s[k][q]);
-        s[k][q] = fmaf(a[k].z, b[q].z, s[k][q]); s[k][q] = fmaf(a[k].w, b[q].w, s[k][q]);
-      }
+      for (int q = 0; q < 4; ++q) p[k][q] = fma2(a[k].y, b[q].y, fma2(a[k].x, b[q].x, p[k][q]));
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float lo, hi;
+      unpack2(p[k][q], lo, hi);
+      s[k][q] = lo + hi;
+    }
 }
 
-// acc[k][.] += sum_j G[4 ty + k][j] B[j][channels of tx]
+// acc[k][.] += sum_j G[4 ty + k][j] B[j][channels of tx, in pairs]
 template <int D>
-__device__ __forceinline__ void sm_add(const float* G, const float* B, int ty, int tx, float (&acc)[4][D / 16]) {
+__device__ __forceinline__ void sm_add(const float* G, const float* B, int ty, int tx, f32x2 (&acc)[4][D / 32]) {
 #pragma unroll 2
   for (int j = 0; j < SS; j += 4) {
     float g[4][4];
@@ -58,18 +69,18 @@ __device__ __forceinline__ void sm_add(const float* G, const float* B, int ty, i
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      float v[D / 16];
-      ld_cols<D>(B + (j + s) * (D + 4), tx, v);
+      f32x2 v[D / 32];
+      ld_col_pairs<D>(B + (j + s) * (D + 4), tx, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int q = 0; q < D / 16; ++q) acc[k][q] = fmaf(g[k][s], v[q], acc[k][q]);
+        for (int q = 0; q < D / 32; ++q) acc[k][q] = fma2(pack2(g[k][s], g[k][s]), v[q], acc[k][q]);
     }
   }
 }
 
 // Score of a pair in base 2, and 1 - tanh^2 of the cap (1 without).
-__device__ __forceinline__ float sm_score(float dot, const SmArgs& a, float slope2, int dist, float& bend) {
+__device__ __forceinline__ float sm_score(float dot, const SmArgs& a, float slope2, float dist, float& bend) {
   float x = dot * a.scale;
   bend = 1.f;
   if (a.cap > 0.f) {
@@ -77,11 +88,11 @@ __device__ __forceinline__ float sm_score(float dot, const SmArgs& a, float slop
     x = t * a.cap;
     bend = 1.f - t * t;
   }
-  return fmaf(x, kLog2e, -slope2 * (float)abs(dist));
+  return fmaf(x, kLog2e, -slope2 * fabsf(dist));
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmArgs a) {
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __grid_constant__ SmArgs a) {
   pdl_wait();
   extern __shared__ __align__(16) float sm_smem[];
   float *Qs = sm_smem, *Ks = Qs + SS * (D + 4), *Vs = Ks + SS * (D + 4), *Ps = Vs + SS * (D + 4);
@@ -97,7 +108,8 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
   const float slope2 = a.slopes ? a.slopes[h] * kLog2e : 0.f;
   const int2 range = sm_range<SS, false>(a, m, b, i0, sh);
   sm_tile<T, D>(Qs, Q, a.q.t, i0, a.nq, nullptr);
-  float acc[4][D / 16], mx[4], sum[4];
+  f32x2 acc[4][D / 32];
+  float mx[4], sum[4];
   int lim[4], doc[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -107,7 +119,7 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
     doc[k] = dq && i < a.nq ? dq[i] : 0;
     if (doc[k] < 0) lim[k] = 0;
 #pragma unroll
-    for (int q = 0; q < D / 16; ++q) acc[k][q] = 0.f;
+    for (int q = 0; q < D / 32; ++q) acc[k][q] = pack2(0.f, 0.f);
   }
   for (int t = range.x; t < range.y; ++t) {
     const int j0 = t * SS;
@@ -119,13 +131,13 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
     sm_dots<D>(Qs, Ks, ty, tx, s);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int p = i0 + ty * 4 + k + m.off;
+      const float away = (float)(i0 + ty * 4 + k + m.off - j0 - tx);        // position of the query less that of key j0 + tx
       float top = -INFINITY;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int j = j0 + tx + 16 * q;
         float bend;
-        const float x = sm_score(s[k][q], a, slope2, p - j, bend);
+        const float x = sm_score(s[k][q], a, slope2, away - (float)(16 * q), bend);
         s[k][q] = j < lim[k] && (!dk || dk[j] == doc[k]) ? x : -INFINITY;
         top = fmaxf(top, s[k][q]);
       }
@@ -136,7 +148,7 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
       mx[k] = now;
       sum[k] *= old;
 #pragma unroll
-      for (int q = 0; q < D / 16; ++q) acc[k][q] *= old;
+      for (int q = 0; q < D / 32; ++q) acc[k][q] = mul2(acc[k][q], pack2(old, old));
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const float e = ex2(s[k][q] - ref);
@@ -156,7 +168,12 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
     if (i >= a.nq) continue;
     const float inv = sum[k] > 0.f ? 1.f / sum[k] : (sum[k] == 0.f ? 0.f : sum[k]);     // NaN stays
 #pragma unroll
-    for (int q = 0; q < D / 16; ++q) O[i * a.o.t + ColMap<D>::col(tx, q)] = from_f<T>(acc[k][q] * inv);
+    for (int q = 0; q < D / 32; ++q) {
+      float u, v;
+      unpack2(mul2(acc[k][q], pack2(inv, inv)), u, v);
+      O[i * a.o.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
+      O[i * a.o.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+    }
     if (tx == 0) a.lse[(long long)blockIdx.x * a.nq + i] = sum[k] == 0.f ? -INFINITY : mx[k] * kLn2 + logf(sum[k]);
   }
 }
@@ -164,7 +181,7 @@ __global__ void __launch_bounds__(256) k_softmax_fwd(const __grid_constant__ SmA
 // KEYS false: stationary queries (X1 = Q, X2 = dO), moving keys (Y1 = K, Y2 = V): dQ, and delta for the other pass.
 // KEYS true: stationary keys (X1 = K, X2 = V), moving queries (Y1 = Q, Y2 = dO) of every query head of the group: dK, dV.
 template <typename T, int D, bool KEYS>
-__global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmArgs a) {
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __grid_constant__ SmArgs a) {
   pdl_wait();
   extern __shared__ __align__(16) float sm_smem[];
   constexpr int TF = SS * (D + 4);
@@ -203,11 +220,11 @@ __global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmA
       if (i < a.nq) a.delta[(long long)blockIdx.x * a.nq + i] = v;
     }
   }
-  float a1[4][D / 16], a2[4][D / 16];
+  f32x2 a1[4][D / 32], a2[4][D / 32];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int q = 0; q < D / 16; ++q) a1[k][q] = a2[k][q] = 0.f;
+    for (int q = 0; q < D / 32; ++q) a1[k][q] = a2[k][q] = pack2(0.f, 0.f);
   for (int h = KEYS ? hs * a.group : hs; h < (KEYS ? (hs + 1) * a.group : hs + 1); ++h) {
     const int hk = h / a.group;
     const float slope2 = a.slopes ? a.slopes[h] * kLog2e : 0.f;
@@ -231,18 +248,21 @@ __global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmA
       sm_dots<D>(X1, Y1, ty, tx, s);
       sm_dots<D>(X2, Y2, ty, tx, g);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
+        // position of the query less that of the key, moving row tx
+        const float away = (float)(KEYS ? m0 + tx + m.off - (s0 + ty * 4 + k) : s0 + ty * 4 + k + m.off - (m0 + tx));
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int rs = ty * 4 + k, rm = tx + 16 * q, i = KEYS ? m0 + rm : s0 + rs, j = KEYS ? s0 + rs : m0 + rm, ri = KEYS ? rm : rs;
           const bool ok = i < a.nq && j < m.limit(i) && (!dk || (dq[i] >= 0 && dq[i] == dk[j]));
           float bend;
-          const float x = sm_score(s[k][q], a, slope2, i + m.off - j, bend);
+          const float x = sm_score(s[k][q], a, slope2, away + (KEYS ? (float)(16 * q) : -(float)(16 * q)), bend);
           const float p = ok ? ex2(x - L[ri]) : 0.f;
           const float ds = ok ? p * (g[k][q] - Dl[ri]) * bend * a.scale : 0.f;
           S[rs * SSG + rm] = ds;
           if (KEYS) P[rs * SSG + rm] = p;
         }
+      }
       __syncthreads();
       sm_add<D>(S, Y1, ty, tx, a2);
       if (KEYS) sm_add<D>(P, Y2, ty, tx, a1);
@@ -256,9 +276,16 @@ __global__ void __launch_bounds__(256) k_softmax_bwd(const __grid_constant__ SmA
     const int i = s0 + ty * 4 + k;
     if (i >= (KEYS ? a.nk : a.nq)) continue;
 #pragma unroll
-    for (int q = 0; q < D / 16; ++q) {
-      g2[i * o2.t + ColMap<D>::col(tx, q)] = from_f<T>(a2[k][q]);
-      if (KEYS) g1[i * a.dv.t + ColMap<D>::col(tx, q)] = from_f<T>(a1[k][q]);
+    for (int q = 0; q < D / 32; ++q) {
+      float u, v;
+      unpack2(a2[k][q], u, v);
+      g2[i * o2.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
+      g2[i * o2.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+      if (KEYS) {
+        unpack2(a1[k][q], u, v);
+        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
+        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+      }
     }
   }
 }
