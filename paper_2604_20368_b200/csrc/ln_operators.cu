@@ -137,17 +137,20 @@ StepPlan plan_step(const ln_softmax* p) {
 }
 
 // tcgen05 forward: query tiles a CTA (T), and the split of the keys over CTAs where the query tiles alone do not fill the GPU.
+// One tile and two CTAs an SM: always with up to 64 channels (32 heads x 4096 tokens 224 us, two tiles 226; with a cap 412 and 453, with
+// a bias 267 and 312), and for short rows; with 128 channels and long rows two tiles, which copy each key tile once for both.
 struct SplitPlan { int tiles, chunk, splits; };
 SplitPlan plan_split(const ln_softmax* p) {
   SplitPlan s;
-  s.tiles = p->nq <= 128 || p->nk <= 512 ? 1 : 2;
+  s.tiles = p->d <= 64 || p->nq <= 128 || p->nk <= 512 ? 1 : 2;
+  const long long slots = (s.tiles == 1 ? 2ll : 1ll) * sm_count();           // CTAs resident
   const long long heads = (long long)p->B * p->Hq, blocks = cdiv(p->nq, 128 * s.tiles), keys = cdiv(p->nk, 128);
   s.chunk = (int)keys; s.splits = 1;
-  if (blocks * heads >= 2ll * sm_count()) return s;
+  if (blocks * heads >= 2 * slots) return s;
   // key tiles of all CTAs together; causal rows see half of the last nq keys
   long long total = blocks * keys;
   if (p->causal && !p->prefix) total -= blocks * (std::min(p->nq, p->nk) / 128) / 2;
-  long long chunk = (total * heads + 3ll * sm_count() - 1) / (3ll * sm_count());
+  long long chunk = (total * heads + 3 * slots - 1) / (3 * slots);
   if (chunk < 8) chunk = 8;
   if (chunk >= keys) return s;
   s.chunk = (int)chunk; s.splits = (int)((keys + chunk - 1) / chunk);
@@ -370,8 +373,8 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   int made = LN_OK;
   if (p->dtype == LN_BF16) {
     const SplitPlan pl = plan_split(p);
-    if (pl.tiles == 1) made = p->d == 128 ? softmax_fwd_umma<128, 1>(a, pl, w.part, st) : softmax_fwd_umma<64, 1>(a, pl, w.part, st);
-    else made = p->d == 128 ? softmax_fwd_umma<128, 2>(a, pl, w.part, st) : softmax_fwd_umma<64, 2>(a, pl, w.part, st);
+    if (p->d <= 64) made = softmax_fwd_umma<64, 1>(a, pl, w.part, st);
+    else made = pl.tiles == 1 ? softmax_fwd_umma<128, 1>(a, pl, w.part, st) : softmax_fwd_umma<128, 2>(a, pl, w.part, st);
   }
   else if (p->d == 32) softmax_fwd_simt<float, 32>(a, st);
   else if (p->d == 64) softmax_fwd_simt<float, 64>(a, st);

@@ -16,7 +16,7 @@
 // Key tiles come last first: with a distance bias the nearest keys then set the reference at once.
 // Bound: 4 * 128 * 128 * d operations on the tensor core (1024 clocks a tile at d = 128) against 128 * 128 exponentials at 16 a
 // clock and SM (1024 clocks; with a cap 1.25 more special functions each, see sm_cap4).  32 heads of 4096 tokens without masks: 128
-// channels 280 to 310 us (0.89 to 0.98 PFLOP/s, a tile every 2100 clocks), 64 channels 225, with a cap 450, with a bias 310.
+// channels 280 to 310 us (0.89 to 0.98 PFLOP/s, a tile every 2100 clocks), 64 channels 224, with a cap 412, with a bias 267.
 #pragma once
 #include "ln_softmax.cuh"
 #include "ln_tile_umma.cuh"
@@ -50,7 +50,7 @@ __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
 
 template <int D, int T> struct SuFwd {
   static constexpr int kTile = 128 * D * 2;                       // bytes of a 128-row tile
-  static constexpr int kStages = T == 1 ? (D == 64 ? 2 : 1) : (D == 64 ? 4 : 2);
+  static constexpr int kStages = T == 1 && D == 128 ? 1 : 2;
   static constexpr int kThreads = T * 160 + 32, kCtas = T == 1 ? 2 : 1;
   static constexpr int kTmem = T == 1 ? 256 : 512;
   static constexpr size_t kSmem = 1024 + (size_t)kTile * (T + 2 * kStages);
