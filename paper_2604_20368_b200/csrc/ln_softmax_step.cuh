@@ -3,9 +3,9 @@
 //
 // Bound by memory traffic: the keys and values of a head, once.  The keys are split over CTAs, over the four warps of a CTA in
 // turns of 16 keys, and every warp keeps maximum, sum and accumulator of its own; warps are joined through shared memory, CTAs
-// by k_softmax_join.  bf16 rows go straight from global memory into the operands of mma.sync (m16n8k16, fp32 accumulate; 16 rows
-// are all a serving step has, a tcgen05 tile would be 128): both products sum over an axis whose order is free, so a lane's
-// 16-byte piece of a row IS its share of an operand, and neither K nor V passes through shared memory.
+// by k_softmax_join.  bf16 rows become the operands of mma.sync as they are (m16n8k16, fp32 accumulate; 16 rows are all a serving step
+// has, a tcgen05 tile would be 128): both products sum over an axis whose order is free, so a lane's 16-byte piece of a row IS its
+// share of an operand, and no lane needs what another one fetched.
 //   S = Q K^T   B = K^T: lane (g, c) = (lane / 4, lane % 4) holds channels 32 l + 8 c .. of key g, which stand for k-steps 2 l, 2 l + 1
 //   O = A V     B = V:   lane (g, c) holds channels 8 g .. (and 64 + 8 g .., or 4 g ..) of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9; column
 //               tile j is channel 8 g + j (then 64 + 8 g + j - 8, or 4 g + j): eight lanes read 128 bytes in a row

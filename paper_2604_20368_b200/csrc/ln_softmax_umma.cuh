@@ -7,8 +7,8 @@
 // Warps 4 t .. 4 t + 3 form the exponentials of tile t, one warp copies, one warp a tile issues the products (a wait costs some 200
 // clocks beside the products' operand reads, and with one warp for both tiles each waited for the other's).  While one tile's
 // exponentials are formed the tensor core works for the other one: of the same CTA (T = 2: each key tile is copied once for both)
-// or of the other CTA on the SM (T = 1, for short rows, where starting and ending a CTA is most of it: 384 heads of 197 tokens
-// 39 -> 31 us).
+// or of the other CTA on the SM (T = 1, with 64 channels, and for short rows, where starting and ending a CTA is most of it: 384
+// heads of 197 tokens 39 -> 31 us).
 // With 64 channels TMEM has room for A beside S: S of the next key tile is formed as soon as this one's is in registers.
 // The reference of a row's exponentials is a maximum that is only renewed when the true one has grown by more than 8 (base 2):
 // the accumulator is then rescaled in TMEM, which is rare; A stays below 2^8, whose rounding to bf16 is the same half step, and
