@@ -352,7 +352,7 @@ int qk_norm_rope_bwd(const ln_rope* p, int32_t B, int32_t n, int32_t Hq, int32_t
  * position p_i = i + len - nq, where len = kv_len[b] (clamped to 0 .. nk) or nk: the last query stands at the last key.
  * A pair is left if j < len, and (causal) j <= p_i or j < prefix[b], and (documents) doc_q[i] == doc_k[j] >= 0.
  * A row with no pair left gets O = 0 and lse = -infinity, and no gradient.  Keys at or behind len, and keys and queries with a
- * negative document (padding), may hold anything, infinities and NaN included: they are never multiplied.  Other masked pairs
+ * negative document (padding), may hold anything, infinities and NaN included: they reach no result.  Other masked pairs
  * are left out of every sum, but share matrix products with pairs that are not: their values have to be finite.
  */
 typedef struct ln_softmax {

@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
     slope2[s] = in && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
 #pragma unroll
     for (int l = 0; l < KL; ++l) {
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (in) v = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.q.p) + b * a.q.b + hq * a.q.h + i * a.q.t + l * 32 + c * 8);
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);                // padding is zeros whatever it holds
+      if (in && doc[s] >= 0) v = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.q.p) + b * a.q.b + hq * a.q.h + i * a.q.t + l * 32 + c * 8);
       qa[s][4 * l] = v.x; qa[s][4 * l + 1] = v.y; qa[s][4 * l + 2] = v.z; qa[s][4 * l + 3] = v.w;
     }
   }
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
   constexpr int NP = step_pieces<D>();
   char* mine = st_smem + (size_t)warp * ST_STAGES * NP * 512 + lane * 16;    // [stage][piece][lane]
   // the 16 keys from j0: lane group g has keys j0 + g and j0 + 8 + g, and values of j0 + 2 c, + 1, + 8, + 9.  Absent ones are zeros
-  // whatever they hold: a value is multiplied by its zero, and a cap's reciprocal is shared by four scores.
+  // whatever they hold: a value is multiplied by its zero, and a cap's reciprocal is shared by four scores of a row.
   auto fetch = [&](int j0, int stage) {
     char* to = mine + stage * NP * 512;
     if (j0 < k1) {
@@ -160,10 +160,15 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
         mma_bf16(s[t], A0, kv.x, kv.y);
         mma_bf16(s[t], A1, kv.z, kv.w);
       }
-    // scores in base 2: lane (g, c) has keys j0 + 8 t + 2 c + e for rows g and g + 8
+    // scores in base 2: lane (g, c) has keys j0 + 8 t + 2 c + e for rows g and g + 8; a reciprocal of the cap serves one row's four,
+    // so that a NaN stays in its row
     if (a.cap > 0.f) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) sm_cap4(s[t], sc.mul);
+      for (int r = 0; r < 2; ++r) {
+        float q[4] = {s[0][2 * r], s[0][2 * r + 1], s[1][2 * r], s[1][2 * r + 1]};
+        sm_cap4(q, sc.mul);
+        s[0][2 * r] = q[0]; s[0][2 * r + 1] = q[1]; s[1][2 * r] = q[2]; s[1][2 * r + 1] = q[3];
+      }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)

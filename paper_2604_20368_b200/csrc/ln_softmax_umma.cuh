@@ -37,7 +37,7 @@ __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
 }
 __device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 // dot products -> r, four at a time with one reciprocal: 1 / u = v / (u v).  exp(2 y) is held at 2^30 (r = 2^-30 there, tanh = 1 to
-// 2^-29), so that a product of four stays in range.  One NaN makes all four NaN: masked products have to be cleared before.
+// 2^-29), so that a product of four stays in range.  One NaN makes all four NaN: they are scores of one row, and masked products are cleared before.
 __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) x[k] = min_nan(x[k] * mul, 30.f);
