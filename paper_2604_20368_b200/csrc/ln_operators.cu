@@ -271,6 +271,14 @@ bool tile_map(const SmView& v, int B, int H, int n, int d, int rows, TileMap* m)
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// f(kind of the cap), a constant
+template <typename F> void by_cap(float cap, const F& f) {
+  const int kind = cap_kind(cap);
+  if (kind == CAP_WIDE) f(std::integral_constant<int, CAP_WIDE>());
+  else if (kind == CAP_USUAL) f(std::integral_constant<int, CAP_USUAL>());
+  else f(std::integral_constant<int, CAP_NONE>());
+}
+
 template <int D, int T> int softmax_fwd_umma(const SmArgs& a, const SplitPlan& pl, const StepPart& part, cudaStream_t st) {
   TileMap q, k, v;
   if (!tile_map(a.q, a.B, a.Hq, a.nq, a.d, 128, &q) || !tile_map(a.k, a.B, a.Hk, a.nk, a.d, 128, &k) || !tile_map(a.v, a.B, a.Hk, a.nk, a.d, 128, &v)) return LN_ERR_CUDA;
@@ -279,8 +287,11 @@ template <int D, int T> int softmax_fwd_umma(const SmArgs& a, const SplitPlan& p
     want_smem(kern, SuFwd<D, T>::kSmem);
     LN_LAUNCH("k_softmax_fwd", st, enqueue(kern, dim3(a.B * a.Hq, cdiv(a.nq, T * 128), pl.splits), SuFwd<D, T>::kThreads, SuFwd<D, T>::kSmem, st, a, q, k, v, sp));
   };
-  if (a.cap > 0.f) { if (a.slopes) go(k_softmax_fwd_umma<D, T, true, true>); else go(k_softmax_fwd_umma<D, T, true, false>); }
-  else { if (a.slopes) go(k_softmax_fwd_umma<D, T, false, true>); else go(k_softmax_fwd_umma<D, T, false, false>); }
+  auto bias = [&](auto cap) {
+    constexpr int C = decltype(cap)::value;
+    if (a.slopes) go(k_softmax_fwd_umma<D, T, C, true>); else go(k_softmax_fwd_umma<D, T, C, false>);
+  };
+  by_cap(a.cap, bias);
   if (pl.splits > 1) softmax_join<bf16>(a, pl.splits, part, st);
   return LN_OK;
 }
@@ -296,13 +307,12 @@ template <int D> int softmax_bwd_umma(const SmArgs& a, cudaStream_t st) {
     want_smem(kv, SuBwd<D>::kSmem);
     LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(kv, dim3(a.B * a.Hk, cdiv(a.nk, 128)), SuBwd<D>::kThreads, SuBwd<D>::kSmem, st, a, sk, sv, mq, mdo));
   };
-  if (a.cap > 0.f) {
-    if (a.slopes) go(k_softmax_bwd_umma<D, true, true, false>, k_softmax_bwd_umma<D, true, true, true>);
-    else go(k_softmax_bwd_umma<D, true, false, false>, k_softmax_bwd_umma<D, true, false, true>);
-  } else {
-    if (a.slopes) go(k_softmax_bwd_umma<D, false, true, false>, k_softmax_bwd_umma<D, false, true, true>);
-    else go(k_softmax_bwd_umma<D, false, false, false>, k_softmax_bwd_umma<D, false, false, true>);
-  }
+  auto bias = [&](auto cap) {
+    constexpr int C = decltype(cap)::value;
+    if (a.slopes) go(k_softmax_bwd_umma<D, C, true, false>, k_softmax_bwd_umma<D, C, true, true>);
+    else go(k_softmax_bwd_umma<D, C, false, false>, k_softmax_bwd_umma<D, C, false, true>);
+  };
+  by_cap(a.cap, bias);
   return LN_OK;
 }
 

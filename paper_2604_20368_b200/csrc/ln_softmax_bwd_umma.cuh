@@ -28,7 +28,7 @@ template <int D> struct SuBwd {
   static constexpr size_t kSmem = 1024 + 2 * (size_t)kX + 2 * (size_t)kY * kStages;
 };
 
-template <int D, bool CAP, bool BIAS, bool KEYS>
+template <int D, int CAP, bool BIAS, bool KEYS>
 __global__ void __launch_bounds__(SuBwd<D>::kThreads, SuBwd<D>::kCtas)
 k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mx1, const __grid_constant__ TileMap mx2,
                    const __grid_constant__ TileMap my1, const __grid_constant__ TileMap my2) {
@@ -202,7 +202,8 @@ k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
     const int* dm = KEYS ? dq : dk;
     const int nm = KEYS ? a.nq : a.nk, buf = group;
     SmScore sc = sm_score_of(a, first_head);
-    const f32x2 ka = pack2(CAP ? -2.f * sc.cap2 : sc.mul, CAP ? -2.f * sc.cap2 : sc.mul), kb = pack2(sc.cap2, sc.cap2);
+    const float down = CAP == CAP_USUAL ? -2.f * sc.cap2 : CAP ? -1.f : sc.mul;
+    const f32x2 ka = pack2(down, down), kb = pack2(sc.cap2, sc.cap2);
     const f32x2 rowL2 = pack2(-rowL, -rowL), rowD2 = pack2(-rowD, -rowD);
     const uint32_t ts = tm + quarter + buf * 128;
     int tile = range.x + group, head = first_head;                            // of moving tile n
@@ -243,14 +244,17 @@ k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
 #pragma unroll
               for (int k = 0; k < 4; ++k)
                 if (!((left >> (e + k)) & 1u)) q[k] = 0.f;
-            sm_cap4(q, sc.mul);
+            if (CAP == CAP_WIDE) sm_cap4_wide(q, sc); else sm_cap4(q, sc.mul);
           }
           float p[4], d[4];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const f32x2 v = pack2(q[2 * k], q[2 * k + 1]);
-            if (CAP) bend[k] = mul2(v, fma2(v, pack2(-4.f, -4.f), pack2(4.f, 4.f)));
-            unpack2(fma2(v, ka, CAP ? add2(kb, L[k]) : L[k]), p[2 * k], p[2 * k + 1]);
+            if (CAP == CAP_WIDE) {                                           // v is a score over the cap, tanh, but for its sign
+              const f32x2 t = mul2(v, pack2(1.f / sc.cap2, 1.f / sc.cap2));
+              bend[k] = fma2(mul2(t, pack2(-1.f, -1.f)), t, pack2(1.f, 1.f));
+            } else if (CAP) bend[k] = mul2(v, fma2(v, pack2(-4.f, -4.f), pack2(4.f, 4.f)));
+            unpack2(fma2(v, ka, CAP == CAP_USUAL ? add2(kb, L[k]) : L[k]), p[2 * k], p[2 * k + 1]);
           }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {

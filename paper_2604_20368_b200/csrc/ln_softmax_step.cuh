@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
     }
   }
   const SmScore sc = sm_score_of(a, hk * a.group);
-  const float ka = a.cap > 0.f ? -2.f * sc.cap2 : sc.mul, kb = a.cap > 0.f ? sc.cap2 : 0.f;
+  const float ka = sc.down, kb = sc.mid;
   const int sure = dk ? 0 : min(k1, m.limit(0));           // every row sees the keys before it (rows that do not exist go nowhere)
   float acc[NT][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -162,11 +162,11 @@ __global__ void __launch_bounds__(ST_WARPS * 32, 2) k_softmax_step(const __grid_
       }
     // scores in base 2: lane (g, c) has keys j0 + 8 t + 2 c + e for rows g and g + 8; a reciprocal of the cap serves one row's four,
     // so that a NaN stays in its row
-    if (a.cap > 0.f) {
+    if (sc.kind != CAP_NONE) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         float q[4] = {s[0][2 * r], s[0][2 * r + 1], s[1][2 * r], s[1][2 * r + 1]};
-        sm_cap4(q, sc.mul);
+        if (sc.kind == CAP_WIDE) sm_cap4_wide(q, sc); else sm_cap4(q, sc.mul);
         s[0][2 * r] = q[0]; s[0][2 * r + 1] = q[1]; s[1][2 * r] = q[2]; s[1][2 * r + 1] = q[3];
       }
     }

@@ -24,15 +24,25 @@
 namespace ln {
 
 __device__ __forceinline__ float min_nan(float x, float y) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
-// Scores in base 2 from the products of scale and cap.  With a cap x = cap log2(e) tanh(y), y = dot scale / cap, and
-// tanh(y) = 1 - 2 r, r = 1 / (exp(2 y) + 1): off by 2^-22 of the cap (an approximate tanh would be off by 2^-11 of it), and
-// 1 - tanh(y)^2 = 4 r (1 - r).
-struct SmScore { float mul, cap2, slope2; };
+// Scores in base 2 from products (dot), through a value x: score = mid + down x.  Without a cap x is the product itself.  With one the
+// score is cap log2(e) tanh(y), y = dot scale / cap, and tanh(y) = 1 - 2 r, x = r = 1 / (exp(2 y) + 1): off by 2^-22 of the cap (an approximate
+// tanh would be off by 2^-11 of it), and 1 - tanh(y)^2 = 4 r (1 - r).  2^-22 of a cap above 128 is more than 2^-15 of a score of one and grows with
+// the cap: there x is the score itself with its sign changed, from the product where y is small (see sm_cap4_wide).
+// A branch on it in the kernels of smaller caps cost those 8 % (128 channels forward 581 -> 628 us), so wide caps have kernels of their own: 32
+// heads of 4096 tokens, 128 channels, forward 823 us where smaller caps take 592, both backward passes 1314 and 1096.
+constexpr float kWideCap = 128.f;
+enum { CAP_NONE = 0, CAP_USUAL = 1, CAP_WIDE = 2 };
+__host__ __device__ __forceinline__ int cap_kind(float cap) { return cap > kWideCap ? CAP_WIDE : cap > 0.f ? CAP_USUAL : CAP_NONE; }
+struct SmScore { float mul, lin, cap2, slope2, down, mid; int kind; };
 __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
   SmScore s;
-  s.mul = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+  s.kind = cap_kind(a.cap);
+  s.lin = a.scale * kLog2e;
+  s.mul = s.kind ? 2.f * kLog2e * a.scale / a.cap : s.lin;
   s.cap2 = a.cap * kLog2e;
   s.slope2 = a.slopes ? a.slopes[h] * kLog2e : 0.f;
+  s.down = s.kind == CAP_USUAL ? -2.f * s.cap2 : s.kind ? -1.f : s.mul;
+  s.mid = s.kind == CAP_USUAL ? s.cap2 : 0.f;
   return s;
 }
 __device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -46,6 +56,38 @@ __device__ __forceinline__ void sm_cap4(float (&x)[4], float mul) {
   const float u = x[0] * x[1], v = x[2] * x[3], r = rcp_fast(u * v), ru = r * v, rv = r * u;
   const float r0 = ru * x[1], r1 = ru * x[0], r2 = rv * x[3], r3 = rv * x[2];
   x[0] = r0; x[1] = r1; x[2] = r2; x[3] = r3;
+}
+
+// dot products -> scores with their sign changed, for wide caps.  Below |y| = 1/2 the score is the uncapped one times tanh(y) / y, its Taylor
+// series to y^14 (remainder 1e-8): a few half steps of the score whatever the cap.  Beyond, cap (1 - 2 r) is as good.  A whole warp: the
+// second form only where some lane needs it (its branch also keeps the compiler from spreading 32 of these over the registers: 728
+// bytes of stack without).
+__device__ __forceinline__ void sm_cap4_wide(float (&x)[4], const SmScore& s) {
+  const float half = s.mul * (0.5f * kLn2);
+  float n[4];
+  bool near = true;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float y = x[k] * half, u = y * y;
+    float p = fmaf(u, -1.4558344e-3f, 3.5921280e-3f);
+    p = fmaf(p, u, -8.8632355e-3f);
+    p = fmaf(p, u, 2.1869488e-2f);
+    p = fmaf(p, u, -5.3968254e-2f);
+    p = fmaf(p, u, 1.3333333e-1f);
+    p = fmaf(p, u, -3.3333333e-1f);
+    p = fmaf(p, u, 1.f);
+    n[k] = -(x[k] * s.lin) * p;
+    near = near && fabsf(y) < 0.5f;
+  }
+  if (!__all_sync(0xffffffffu, near)) {
+    float r[4] = {x[0], x[1], x[2], x[3]};
+    sm_cap4(r, s.mul);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (!(fabsf(x[k] * half) < 0.5f)) n[k] = fmaf(2.f * r[k], s.cap2, -s.cap2);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = n[k];
 }
 
 template <int D, int T> struct SuFwd {
@@ -93,7 +135,7 @@ __device__ __forceinline__ uint32_t sm_left(int from, int to, const int* dm, int
 // Keys are split over CTAs (blockIdx.z) where the query tiles alone do not fill the GPU: a CTA takes `chunk` of its key tiles.
 struct SmSplit { int chunk, splits; float* o; float2* ml; };       // parts: [row][split][d], maximum (base 2) and sum
 
-template <int D, int T, bool CAP, bool BIAS>
+template <int D, int T, int CAP, bool BIAS>
 __global__ void __launch_bounds__(SuFwd<D, T>::kThreads, SuFwd<D, T>::kCtas)
 k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ TileMap mq, const __grid_constant__ TileMap mk,
                    const __grid_constant__ TileMap mv, const __grid_constant__ SmSplit sp) {
@@ -251,8 +293,9 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         __syncwarp();
         if (lane == 0) umma::mbar_arrive(&s_read[t]);
       }
-      // x: products, r of the cap, or scores with a bias; the score in base 2 is x ka + kb
-      const float ka = BIAS ? 1.f : (CAP ? -2.f * sc.cap2 : sc.mul), kb = CAP && !BIAS ? sc.cap2 : 0.f;
+      // x: products, what stands for a capped score (SmScore), or scores with a bias; the score in base 2 is x ka + kb
+      const float down = CAP == CAP_USUAL ? -2.f * sc.cap2 : CAP ? -1.f : sc.mul, mid = CAP == CAP_USUAL ? sc.cap2 : 0.f;
+      const float ka = BIAS ? 1.f : down, kb = BIAS ? 0.f : mid;
       if (CAP) {
         if (!whole)
 #pragma unroll
@@ -261,7 +304,7 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
 #pragma unroll
         for (int e = 0; e < 128; e += 4) {
           float q[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
-          sm_cap4(q, sc.mul);
+          if (CAP == CAP_WIDE) sm_cap4_wide(q, sc); else sm_cap4(q, sc.mul);
 #pragma unroll
           for (int k = 0; k < 4; ++k) x[e + k] = q[k];
         }
@@ -271,10 +314,10 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
 #pragma unroll
         for (int e = 0; e < 128; ++e) {
           const float far = sc.slope2 * fabsf(p - (float)e);
-          x[e] = CAP ? fmaf(-2.f * sc.cap2, x[e], sc.cap2 - far) : fmaf(x[e], sc.mul, -far);
+          x[e] = fmaf(down, x[e], CAP == CAP_USUAL ? mid - far : -far);
         }
       }
-      constexpr bool DOWN = CAP && !BIAS;                                    // the largest score has the smallest x
+      constexpr bool DOWN = CAP != CAP_NONE && !BIAS;                                    // the largest score has the smallest x
       if (!whole)
 #pragma unroll
         for (int e = 0; e < 128; ++e)

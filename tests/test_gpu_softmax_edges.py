@@ -1,9 +1,11 @@
-"""Softmax attention where rows share a register, a reciprocal or a tile: queries of padding and queries that hold NaN in a step."""
+"""Softmax attention where rows share a register, a reciprocal or a tile: queries of padding and queries that hold NaN in a step;
+caps far above the scores."""
 import math
 
 import pytest
 import torch
 
+from attention_reference import attention, check
 from test_gpu_softmax import BF, DEV, F32, _compare, _inputs, _run, _slopes
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +48,29 @@ def test_a_query_that_holds_nan_spoils_its_own_row_only(dtype, Hq, nq, cap):
     for k in ("O", "lse"):
         got[k][0, h, i] = ref[k][0, h, i]
         assert torch.equal(got[k], ref[k]), k
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d,nq,nk", [(64, 1, 700), (128, 12, 700), (32, 90, 90), (64, 200, 700), (128, 200, 700)])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("cap", [1e4, 1e6, 1e9, 3e38])
+def test_a_large_cap_tends_to_no_cap(dtype, d, nq, nk, bias, cap):
+    """The tolerance is that of uncapped scores: s (1 - (s / cap)^2 / 3) differs from s by 3e-6 of it where |s| < 30 and the cap is 1e4, in
+    the reference as in the kernel; the factor of the cap costs a kernel a few half steps of the score, not of the cap.  (1 - tanh^2 is off by a
+    half step or two of 32 bits, beside the four that a gradient's tolerance has.)"""
+    Q, K, V, dO = _inputs(2, 2, 1, nq, nk, d, dtype, sigma=4.0)
+    kw = dict(causal=True, slopes=_slopes(2) if bias else None)
+    got = _run(Q, K, V, dO, cap=cap, **kw)
+    val, _ = attention(Q, K, V, dO, dtype=dtype, cap=cap, **kw)
+    _, tol = attention(Q, K, V, dO, dtype=dtype, **kw)
+    print(check(got, val, tol))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d,nq,nk", [(64, 3, 700), (64, 200, 700), (128, 200, 700)])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("cap", [100.0, 128.0, 129.0, 1000.0])
+def test_scores_on_both_sides_of_the_cap(dtype, d, nq, nk, bias, cap):
+    Q, K, V, dO = _inputs(1, 2, 2, nq, nk, d, dtype, sigma=0.7 * cap)
+    Q[:, :, ::3] *= 0.01
+    _compare(Q, K, V, dO, causal=True, cap=cap, slopes=_slopes(2) if bias else None)
