@@ -38,7 +38,7 @@ __device__ __forceinline__ SmScore sm_score_of(const SmArgs& a, int h) {
   SmScore s;
   s.kind = cap_kind(a.cap);
   s.lin = a.scale * kLog2e;
-  s.mul = s.kind ? 2.f * kLog2e * a.scale / a.cap : s.lin;
+  s.mul = s.kind ? fminf(2.f * kLog2e * a.scale / a.cap, 3.4028235e38f) : s.lin;     // finite: a product of zero has to stay zero
   s.cap2 = a.cap * kLog2e;
   s.slope2 = a.slopes ? a.slopes[h] * kLog2e : 0.f;
   s.down = s.kind == CAP_USUAL ? -2.f * s.cap2 : s.kind ? -1.f : s.mul;

@@ -1,5 +1,5 @@
 """Softmax attention where rows share a register, a reciprocal or a tile: queries of padding and queries that hold NaN in a step;
-caps far above the scores."""
+caps far above and far below the scores."""
 import math
 
 import pytest
@@ -74,3 +74,16 @@ def test_scores_on_both_sides_of_the_cap(dtype, d, nq, nk, bias, cap):
     Q, K, V, dO = _inputs(1, 2, 2, nq, nk, d, dtype, sigma=0.7 * cap)
     Q[:, :, ::3] *= 0.01
     _compare(Q, K, V, dO, causal=True, cap=cap, slopes=_slopes(2) if bias else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("nq", [1, 150])
+@pytest.mark.parametrize("cap", [1e-30, 1e-39])
+def test_a_tiny_cap_leaves_equal_weights(dtype, nq, cap):
+    Q, K, V, dO = _inputs(1, 2, 2, nq, 300, 64, dtype)
+    Q[:, 0, 0] = 0.0                                           # products of zero: tanh(0) whatever the cap
+    got = _run(Q, K, V, dO, cap=cap)
+    val, tol = attention(Q, K, V, dtype=dtype, cap=cap)
+    check({k: got[k] for k in ("O", "lse")}, val, tol)
+    for k in ("dQ", "dK", "dV"):
+        assert torch.isfinite(got[k]).all(), k
