@@ -1,5 +1,5 @@
 """Softmax attention where rows share a register, a reciprocal or a tile: queries of padding and queries that hold NaN in a step;
-caps far above and far below the scores."""
+caps far above and far below the scores; long rows of 128 channels, the kernel with two query tiles a CTA."""
 import math
 
 import pytest
@@ -87,3 +87,72 @@ def test_a_tiny_cap_leaves_equal_weights(dtype, nq, cap):
     check({k: got[k] for k in ("O", "lse")}, val, tol)
     for k in ("dQ", "dK", "dV"):
         assert torch.isfinite(got[k]).all(), k
+
+
+def _underflow(Q, K, V, dO):
+    """What A and ds below 2^-126, the smallest normal number of 32 bits (and of bf16), may take from the gradients: far from its query a key with a
+    distance bias has nothing else.  Either may come out as zero.  A pair of dV then misses 2^-126 |dO|; one of dK or dQ misses scale
+    2^-126 (1 + |dP - delta|) of its query or key, and |dP - delta| <= 2 |dO|_2 |V|_2 since O is a mean of the V (the cap's factor is at most 1)."""
+    q, k, v, g = (t.cpu().double().abs() for t in (Q, K, V, dO))
+    reach = 2.0 ** -126 / math.sqrt(q.shape[-1]) * (1 + 2 * float(g.norm(dim=-1).max() * v.norm(dim=-1).max()))
+    group = q.shape[1] // k.shape[1]
+    per_key_head = lambda t: t.sum(2, keepdim=True).unflatten(1, (-1, group)).sum(2)
+    per_query_head = lambda t: t.sum(2, keepdim=True).repeat_interleave(group, 1)
+    return dict(dQ=reach * per_query_head(k), dK=reach * per_key_head(q), dV=2.0 ** -126 * per_key_head(g))
+
+
+WIDE = [(1, 2, 513, 513), (2, 2, 129, 1030), (1, 2, 300, 2100), (1, 1, 700, 900)]
+
+
+@pytest.mark.parametrize("B,H,nq,nk", WIDE)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
+@pytest.mark.parametrize("bias", [False, True])
+def test_long_rows_of_wide_heads(B, H, nq, nk, causal, cap, bias):
+    """128 channels, more than 128 queries and 512 keys: two query tiles a CTA, and beyond 1024 keys parts that are joined."""
+    kw = dict(causal=causal, cap=cap, slopes=_slopes(2 * H) if bias else None)
+    if causal and bias:
+        kw["prefix"] = torch.full((B,), nk // 3, dtype=torch.int32)
+    x = _inputs(B, 2 * H, H, nq, nk, 128, BF, sigma=2.0)
+    got = _run(*x, **kw)
+    val, tol = attention(*x, dtype=BF, **kw)
+    for k, t in _underflow(*x).items():
+        tol[k] += t
+    print(check(got, val, tol))
+
+
+@pytest.mark.parametrize("n", [700, 1333])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
+def test_documents_in_long_rows_of_wide_heads(n, cap):
+    Q, K, V, dO = _inputs(2, 2, 1, n, n, 128, BF, packed=True)
+    at = torch.arange(n)
+    doc = torch.stack([at // 290, torch.where(at < n - 200, at // 517, -1)]).int()
+    kw = dict(doc_q=doc, doc_k=doc, causal=True, cap=cap)
+    got = _compare(Q, K, V, dO, **kw)
+    pad = (doc < 0).to(DEV)
+    for t in (Q, K, V, dO):
+        t.transpose(1, 2)[pad] = math.nan
+    again = _run(Q, K, V, dO, **kw)
+    for k in got:
+        assert torch.equal(got[k], again[k]), k
+
+
+@pytest.mark.parametrize("nq,nk", [(150, 600), (400, 1500)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_filled_length_in_long_rows_of_wide_heads(nq, nk, causal):
+    Q, K, V, dO = _inputs(5, 2, 2, nq, nk, 128, BF)
+    kv = torch.tensor([nk, 0, 1, nk - 129, 520], dtype=torch.int32)
+    kw = dict(kv_len=kv, causal=causal, cap=10.0, slopes=_slopes(2))
+    got = _compare(Q, K, V, dO, **kw)
+    for b, n in enumerate(kv.tolist()):
+        K[b, :, n:] = math.nan
+        V[b, :, n:] = math.inf
+    again = _run(Q, K, V, dO, **kw)
+    for k in got:
+        assert torch.equal(got[k], again[k]), k
+
+
+def test_long_rows_of_many_wide_heads():
+    """Query tiles fill the GPU: two tiles a CTA, keys not split."""
+    Q, K, V, _ = _inputs(4, 40, 10, 300, 1100, 128, BF)
+    _compare(Q, K, V, causal=True)
