@@ -74,7 +74,7 @@ k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         umma::tile_load(umma::s32(sX) + XB + blk * 16384, &mx2.map, blk * 64, s0, hs * mx2.head, b * mx2.batch, &x_full);
       }
     }
-    int raw = 0, n = 0;
+    int raw = 0, n = 0;                                                      // copies begun: rows to be cleared first, all tiles
     for (; n < total; ++n) {
       const int s = n % NS, m0 = (range.x + n % nt) * 64, hq = first_head + n / nt, hy = KEYS ? hq : hs / a.group;
       if (n >= NS) ok = warp_wait(&y_free[s], (uint32_t)(n / NS - 1) & 1);
@@ -115,9 +115,11 @@ k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         if (!ok) { ++n; break; }
       }
     }
-    if (!ok)                                                                 // no copy is in flight when the CTA ends
-      for (int s = 0; s < NS; ++s)
-        if (n > s) umma::mbar_wait(&y_full[s], (uint32_t)((n - 1 - s) / NS) & 1);
+    // no copy is in flight when the CTA ends, whichever wait of whichever warp ran out
+    if (total > 0) umma::mbar_wait(&x_full, 0);
+    if (raw > 0) umma::mbar_wait(&y_raw, (uint32_t)(raw - 1) & 1);
+    for (int s = 0; s < NS; ++s)
+      if (n > s) umma::mbar_wait(&y_full[s], (uint32_t)((n - 1 - s) / NS) & 1);
   } else if (warp == MMA) {                                                    // products
     if (umma::elect_one() && total > 0) {
       const uint32_t id_s = umma::instr_desc(64, false, false), id_a = umma::instr_desc(D, false, true);
@@ -159,7 +161,8 @@ k_softmax_bwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         if (n + NB < total) scores(n + NB);
       }
       if (ok) umma::commit(&acc_full);
-      else { umma::commit(&spare); umma::mbar_wait(&spare, 0); }             // no product is in flight when the CTA ends
+      umma::commit(&spare);                                                  // no product is in flight when the CTA ends
+      umma::mbar_wait(&spare, 0);
     }
   } else {                                                                   // exponentials
     const int group = warp >> 2, row = (warp & 3) * 32 + lane, r = s0 + row;

@@ -192,8 +192,8 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         for (int blk = 0; blk < D / 64; ++blk)
           umma::tile_load(umma::s32(sQ) + t * TB + blk * 16384, &mq.map, blk * 64, i0 + t * 128, qh, qb, &q_full);
     }
-    int raw = 0, j = 0;
-    for (; j < nt && ok; ++j) {
+    int raw = 0, ks = 0, vs = 0;                                             // copies begun: rows to be cleared first, K and V tiles
+    for (int j = 0; j < nt && ok; ++j) {
       const int s = j % NS, j0 = k0 + (nt - 1 - j) * 128;
       const uint32_t again = (uint32_t)(j / NS - 1) & 1;
       if (j >= NS) ok = warp_wait(&k_free[s], again);
@@ -203,6 +203,7 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         for (int blk = 0; blk < D / 64; ++blk)
           umma::tile_load(umma::s32(sK) + s * TB + blk * 16384, &mk.map, blk * 64, j0, kh, kb, &k_full[s]);
       }
+      if (ok) ++ks;
       if (j >= NS && ok) ok = warp_wait(&v_free[s], again);
       if (!ok) break;
       // a value row that no query uses may hold an infinity: rows behind the filled length, and padding, become zeros
@@ -215,18 +216,20 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         for (int blk = 0; blk < D / 64; ++blk)
           umma::tile_load(umma::s32(sV) + s * TB + blk * 16384, &mv.map, blk * 64, j0, vh, vb, bar);
       }
+      ++vs;
       if (clear) {
         ok = warp_wait(&v_raw, raw++ & 1);
         tile_clear<D>(sV + s * TB, 128, [&](int r) { const int key = j0 + r; return key >= a.nk || (key < m.len && !(dk && dk[key] < 0)); });
         if (one) umma::mbar_arrive(&v_full[s]);
       }
     }
-    if (!ok)                                                                 // no copy is in flight when the CTA ends
-      for (int s = 0; s < NS; ++s) {
-        const int last = (j - 1 - s) / NS;                                   // uses of stage s so far, less one
-        if (j > s) { umma::mbar_wait(&k_full[s], last & 1); umma::mbar_wait(&v_full[s], last & 1); }
-        if (j % NS == s && j < nt) umma::mbar_wait(&k_full[s], (j / NS) & 1, 1 << 12);
-      }
+    // no copy is in flight when the CTA ends, whichever wait of whichever warp ran out
+    if (nt > 0) umma::mbar_wait(&q_full, 0);
+    if (raw > 0) umma::mbar_wait(&v_raw, (uint32_t)(raw - 1) & 1);
+    for (int s = 0; s < NS; ++s) {
+      if (ks > s) umma::mbar_wait(&k_full[s], (uint32_t)((ks - 1 - s) / NS) & 1);
+      if (vs > s) umma::mbar_wait(&v_full[s], (uint32_t)((vs - 1 - s) / NS) & 1);
+    }
   } else if (warp >= MMA) {                                                  // products of tile t
     if (umma::elect_one() && nt > 0) {
       const int t = warp - MMA;
@@ -262,7 +265,8 @@ k_softmax_fwd_umma(const __grid_constant__ SmArgs a, const __grid_constant__ Til
         if (j + NS < nt) umma::commit(&v_free[s]);
         if (!EARLY && j + 1 < nt) scores(j + 1);
       }
-      if (!ok) { umma::commit(&spare[t]); umma::mbar_wait(&spare[t], 0); }    // no product is in flight when the CTA ends
+      umma::commit(&spare[t]);                                               // nor a product
+      umma::mbar_wait(&spare[t], 0);
     }
   } else {                                                                   // exponentials
     const int t = warp >> 2, lane = tid & 31, row = (warp & 3) * 32 + lane, i = i0 + t * 128 + row;
