@@ -584,7 +584,17 @@ class Rope:
         # floor(2^64 frac(f / 2 pi)) in the 64-bit mantissa of x86's extended precision
         part = f.astype(np.longdouble) / _TWO_PI % 1 * np.longdouble(2) ** 64
         self.turns = torch.from_numpy(part.astype(np.uint64).view(np.int64)).to(device) if f.size else None
+        self._make_plan()
+
+    def _make_plan(self):
         self.plan = marshal().RopePlan(self.d, self.r, self.interleaved, self.factor, self.turns)
+
+    def __getstate__(self):                        # copies and pickles hold the fields; the plan is made again from them
+        return {k: v for k, v in self.__dict__.items() if k != "plan"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._make_plan()
 
 
 def rope_fwd(rope: Rope, Q, K=None, pos=None, start: int = 0, Qr=None, Kr=None, stream=None):
@@ -631,6 +641,13 @@ class SoftmaxAttention:
     def __post_init__(self):
         plan = marshal().SmPlan(self.scale, self.cap, self.causal, self.prefix, self.slopes, self.doc_q, self.doc_k, self.kv_len)
         object.__setattr__(self, "plan", plan)
+
+    def __getstate__(self):                        # as in Rope
+        return {k: v for k, v in self.__dict__.items() if k != "plan"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self.__post_init__()
 
 
 def softmax_attention_workspace_bytes(sp: SoftmaxAttention, Q, K, backward: bool) -> int:
