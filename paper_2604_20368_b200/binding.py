@@ -583,6 +583,7 @@ class Rope:
         self.d, self.r, self.interleaved, self.factor = int(d), 2 * f.size, bool(interleaved), float(factor)
         # floor(2^64 frac(f / 2 pi)) in the 64-bit mantissa of x86's extended precision
         part = f.astype(np.longdouble) / _TWO_PI % 1 * np.longdouble(2) ** 64
+        part[part >= np.longdouble(2) ** 64] = 0       # a fraction that rounds to a whole turn
         self.turns = torch.from_numpy(part.astype(np.uint64).view(np.int64)).to(device) if f.size else None
         self._make_plan()
 

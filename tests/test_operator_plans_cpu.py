@@ -56,3 +56,12 @@ def test_a_model_that_holds_plans_is_copied_whole():
     other = copy.deepcopy(layer)
     assert torch.equal(other.rope.turns, layer.rope.turns) and other.rope.turns.data_ptr() != layer.rope.turns.data_ptr()
     assert other.attention.causal
+
+
+@pytest.mark.filterwarnings("error")
+def test_a_frequency_just_below_zero_is_a_whole_turn():
+    """-1e-30 radians are 1 - 1.6e-31 turns, which the 64 bits of the table's arithmetic round to one turn: the fraction is 0 or 2^64 - 1."""
+    rope = ln.Rope(64, [-1e-30, -1e-19, 1e-30, -0.25, 0.25])
+    t = [x % 2 ** 64 for x in rope.turns.tolist()]
+    assert min(t[0], 2 ** 64 - t[0]) <= 1 and min(t[1], 2 ** 64 - t[1]) <= 1 and t[2] == 0
+    assert abs((t[3] + t[4]) - 2 ** 64) <= 1
