@@ -1,6 +1,7 @@
 """Build the sm_100a shared library in-tree (nvcc cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import contextlib
 import glob
 import os
 import re
@@ -38,6 +39,17 @@ def _depends(path: str, seen=None):
     return seen
 
 
+@contextlib.contextmanager
+def _discarding(paths):
+    """Those of the paths that still exist at the end are removed: what a compile that failed, or was interrupted, wrote."""
+    try:
+        yield
+    finally:
+        for p in paths:
+            if os.path.exists(p):
+                os.remove(p)
+
+
 def _newest(paths) -> float:
     return max(os.path.getmtime(p) for p in paths)
 
@@ -55,20 +67,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     os.makedirs(OBJ_DIR, exist_ok=True)
     tag = f".tmp{os.getpid()}"
-    objects, running = [], []
-    for src in sources():
-        obj = os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o")
-        objects.append(obj)
-        if force or not os.path.exists(obj) or _newest(_depends(src)) > os.path.getmtime(obj):
-            cmd = ["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj + tag, src]
-            running.append((subprocess.Popen(cmd), cmd, obj))
-    failed = [cmd for proc, cmd, _ in running if proc.wait() != 0]
-    if failed:
-        raise subprocess.CalledProcessError(1, failed[0])
-    for _, _, obj in running:
-        os.replace(obj + tag, obj)
-    subprocess.check_call(["nvcc"] + NVCC_FLAGS + ["-shared", "-o", LIB + tag] + objects)
-    os.replace(LIB + tag, LIB)
+    objects = [os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o") for src in sources()]
+    running = []
+    with _discarding([p + tag for p in objects + [LIB]]):
+        for src, obj in zip(sources(), objects):
+            if force or not os.path.exists(obj) or _newest(_depends(src)) > os.path.getmtime(obj):
+                cmd = ["nvcc"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj + tag, src]
+                running.append((subprocess.Popen(cmd), cmd, obj))
+        failed = [cmd for proc, cmd, _ in running if proc.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        for _, _, obj in running:
+            os.replace(obj + tag, obj)
+        subprocess.check_call(["nvcc"] + NVCC_FLAGS + ["-shared", "-o", LIB + tag] + objects)
+        os.replace(LIB + tag, LIB)
     return LIB
 
 
@@ -87,11 +99,12 @@ def build_marshal(force: bool = False) -> str:
                os.path.join(cuda, "include")]
     lib = os.path.join(torch_dir, "lib")
     tmp = MARSHAL + f".tmp{os.getpid()}"
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_EXTENSION_NAME=_ln_torch",
-                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
-                          + [f for d in include for f in ("-isystem" if d != include[0] else "-I", d)]
-                          + [src, "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
-    os.replace(tmp, MARSHAL)
+    with _discarding([tmp]):
+        subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_EXTENSION_NAME=_ln_torch",
+                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+                              + [f for d in include for f in ("-isystem" if d != include[0] else "-I", d)]
+                              + [src, "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+        os.replace(tmp, MARSHAL)
     return MARSHAL
 
 
