@@ -504,7 +504,7 @@ def marshal():
     impossible."""
     global _marshal
     if _marshal is None:
-        path = _build.MARSHAL
+        path = _build.marshal_path()
         try:
             path = _build.build_marshal()
         except Exception as e:   # no compiler on this machine: use the module that travelled with the tree

@@ -14,7 +14,6 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "liblaplace_nystrom.so")
 OBJ_DIR = os.path.join(LIB_DIR, "obj")
-MARSHAL = os.path.join(LIB_DIR, "_ln_torch.so")      # argument marshalling for torch tensors, a Python module
 ROOT = os.path.dirname(HERE)
 
 NVCC_FLAGS = [
@@ -84,13 +83,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
-def build_marshal(force: bool = False) -> str:
-    """Compile csrc/ln_torch.cpp against torch's headers into lib/_ln_torch.so if it or a file it includes changed."""
+def marshal_path() -> str:
+    """The Python module that marshals torch tensors.  It is linked against torch's C++ classes and Python's, so its name holds the
+    versions that it was built for."""
     import torch
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    return os.path.join(LIB_DIR, f"_ln_torch.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}-abi{abi}.so")
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compile csrc/ln_torch.cpp against torch's headers into marshal_path() if it or a file it includes changed."""
+    import torch
+    marshal = marshal_path()
     src = os.path.join(CSRC, "ln_torch.cpp")
     header = os.path.join(ROOT, "include", "laplace_nystrom.h")
-    if not force and os.path.exists(MARSHAL) and _newest([src, header]) <= os.path.getmtime(MARSHAL):
-        return MARSHAL
+    if not force and os.path.exists(marshal) and _newest([src, header]) <= os.path.getmtime(marshal):
+        return marshal
     os.makedirs(LIB_DIR, exist_ok=True)
     torch_dir = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")))
@@ -98,14 +106,14 @@ def build_marshal(force: bool = False) -> str:
                os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
                os.path.join(cuda, "include")]
     lib = os.path.join(torch_dir, "lib")
-    tmp = MARSHAL + f".tmp{os.getpid()}"
+    tmp = marshal + f".tmp{os.getpid()}"
     with _discarding([tmp]):
         subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_EXTENSION_NAME=_ln_torch",
                                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
                               + [f for d in include for f in ("-isystem" if d != include[0] else "-I", d)]
                               + [src, "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
-        os.replace(tmp, MARSHAL)
-    return MARSHAL
+        os.replace(tmp, marshal)
+    return marshal
 
 
 if __name__ == "__main__":

@@ -40,8 +40,6 @@ def test_a_library_that_does_not_link_leaves_only_objects(tree):
 
 
 def test_marshalling_that_does_not_compile_leaves_nothing_behind(tree, monkeypatch):
-    monkeypatch.setattr(build, "MARSHAL", str(tree / "lib" / "_ln_torch.so"))
-
     def fails(cmd):
         open(cmd[cmd.index("-o") + 1], "w").close()
         raise subprocess.CalledProcessError(1, cmd)
@@ -50,3 +48,28 @@ def test_marshalling_that_does_not_compile_leaves_nothing_behind(tree, monkeypat
     with pytest.raises(subprocess.CalledProcessError):
         build.build_marshal()
     assert _files(tree) == []
+
+
+def test_marshalling_belongs_to_one_torch_and_one_python(tree, monkeypatch):
+    """A module built against another torch or Python is not taken: classes may be laid out differently."""
+    import sysconfig
+
+    import torch
+    made = []
+
+    def makes(cmd):
+        made.append(cmd[cmd.index("-o") + 1])
+        open(made[-1], "w").close()
+    src, header = tree / "csrc" / "ln_torch.cpp", os.path.join(build.ROOT, "include", "laplace_nystrom.h")
+    src.write_text("")
+    for f in (src, header):
+        assert os.path.exists(f)
+    monkeypatch.setattr(subprocess, "check_call", makes)
+    first = build.build_marshal()
+    assert build.build_marshal() == first and len(made) == 1           # up to date
+    monkeypatch.setattr(torch, "__version__", "9.9.9")
+    second = build.build_marshal()
+    assert second != first and len(made) == 2 and build.build_marshal() == second and len(made) == 2
+    soabi = sysconfig.get_config_var
+    monkeypatch.setattr(sysconfig, "get_config_var", lambda name: "cpython-999" if name == "SOABI" else soabi(name))
+    assert build.build_marshal() not in (first, second) and len(made) == 3
