@@ -235,15 +235,15 @@ void softmax_step(const ln_softmax* p, const SmArgs& a, const SmWork& w, cudaStr
   if (p->dtype == LN_BF16) softmax_join<bf16>(a, s.splits, w.part, st); else softmax_join<float>(a, s.splits, w.part, st);
 }
 
-template <typename T, int D> void softmax_fwd_simt(const SmArgs& a, cudaStream_t st) {
-  want_smem(k_softmax_fwd<T, D>, sm_fwd_smem<D>());
-  LN_LAUNCH("k_softmax_fwd", st, enqueue(k_softmax_fwd<T, D>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_fwd_smem<D>(), st, a));
+template <int D> void softmax_fwd_simt(const SmArgs& a, cudaStream_t st) {
+  want_smem(k_softmax_fwd<D>, sm_fwd_smem<D>());
+  LN_LAUNCH("k_softmax_fwd", st, enqueue(k_softmax_fwd<D>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_fwd_smem<D>(), st, a));
 }
-template <typename T, int D> void softmax_bwd_simt(const SmArgs& a, cudaStream_t st) {
-  want_smem(k_softmax_bwd<T, D, false>, sm_bwd_smem<D, false>());
-  LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<T, D, false>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_bwd_smem<D, false>(), st, a));
-  want_smem(k_softmax_bwd<T, D, true>, sm_bwd_smem<D, true>());
-  LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<T, D, true>, dim3(a.B * a.Hk, cdiv(a.nk, SS)), 256, sm_bwd_smem<D, true>(), st, a));
+template <int D> void softmax_bwd_simt(const SmArgs& a, cudaStream_t st) {
+  want_smem(k_softmax_bwd<D, false>, sm_bwd_smem<D, false>());
+  LN_LAUNCH("k_softmax_bwd_q", st, enqueue(k_softmax_bwd<D, false>, dim3(a.B * a.Hq, cdiv(a.nq, SS)), 256, sm_bwd_smem<D, false>(), st, a));
+  want_smem(k_softmax_bwd<D, true>, sm_bwd_smem<D, true>());
+  LN_LAUNCH("k_softmax_bwd_kv", st, enqueue(k_softmax_bwd<D, true>, dim3(a.B * a.Hk, cdiv(a.nk, SS)), 256, sm_bwd_smem<D, true>(), st, a));
 }
 
 // The driver's encoder of tensor maps, by name (the library is not linked against the driver).
@@ -386,9 +386,9 @@ int softmax_attention_fwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
     if (p->d <= 64) made = softmax_fwd_umma<64, 1>(a, pl, w.part, st);
     else made = pl.tiles == 1 ? softmax_fwd_umma<128, 1>(a, pl, w.part, st) : softmax_fwd_umma<128, 2>(a, pl, w.part, st);
   }
-  else if (p->d == 32) softmax_fwd_simt<float, 32>(a, st);
-  else if (p->d == 64) softmax_fwd_simt<float, 64>(a, st);
-  else softmax_fwd_simt<float, 128>(a, st);
+  else if (p->d == 32) softmax_fwd_simt<32>(a, st);
+  else if (p->d == 64) softmax_fwd_simt<64>(a, st);
+  else softmax_fwd_simt<128>(a, st);
   const int launched = launch_ok();
   return made != LN_OK ? made : launched;
 }
@@ -410,9 +410,9 @@ int softmax_attention_bwd(const ln_softmax* p, const ln_view* Q, const ln_view* 
   softmax_docs(a, w, st);
   int made = LN_OK;
   if (p->dtype == LN_BF16) made = p->d == 128 ? softmax_bwd_umma<128>(a, st) : softmax_bwd_umma<64>(a, st);
-  else if (p->d == 32) softmax_bwd_simt<float, 32>(a, st);
-  else if (p->d == 64) softmax_bwd_simt<float, 64>(a, st);
-  else softmax_bwd_simt<float, 128>(a, st);
+  else if (p->d == 32) softmax_bwd_simt<32>(a, st);
+  else if (p->d == 64) softmax_bwd_simt<64>(a, st);
+  else softmax_bwd_simt<128>(a, st);
   const int launched = launch_ok();
   return made != LN_OK ? made : launched;
 }

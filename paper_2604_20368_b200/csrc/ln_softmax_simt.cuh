@@ -15,8 +15,8 @@ template <int D, bool KEYS> __host__ __device__ constexpr size_t sm_bwd_smem() {
 
 // 64 rows of a [n, d] slab (row r0 first) into a tile with pitch D + 4; rows at or behind n and rows of padding are zero
 // whatever they hold.
-template <typename T, int D>
-__device__ __forceinline__ void sm_tile(float* dst, const T* src, long long stride, int r0, int n, const int* doc) {
+template <int D>
+__device__ __forceinline__ void sm_tile(float* dst, const float* src, long long stride, int r0, int n, const int* doc) {
   for (int idx = threadIdx.x; idx < SS * (D / 4); idx += 256) {
     const int r = idx / (D / 4), c = idx % (D / 4) * 4, i = r0 + r;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -91,7 +91,7 @@ __device__ __forceinline__ float sm_score(float dot, const SmArgs& a, float slop
   return fmaf(x, kLog2e, -slope2 * fabsf(dist));
 }
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __grid_constant__ SmArgs a) {
   pdl_wait();
   extern __shared__ __align__(16) float sm_smem[];
@@ -99,15 +99,15 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __g
   __shared__ int sh[2];
   const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, hk = h / a.group;
   const int i0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * SS, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;   // long causal rows first
-  const T* Q = static_cast<const T*>(a.q.p) + b * a.q.b + h * a.q.h;
-  const T* K = static_cast<const T*>(a.k.p) + b * a.k.b + hk * a.k.h;
-  const T* V = static_cast<const T*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const float* Q = static_cast<const float*>(a.q.p) + b * a.q.b + h * a.q.h;
+  const float* K = static_cast<const float*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const float* V = static_cast<const float*>(a.v.p) + b * a.v.b + hk * a.v.h;
   const SmMask m(a, b);
   const int* dq = a.doc_q ? a.doc_q + (long long)b * a.nq : nullptr;
   const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
   const float slope2 = a.slopes ? a.slopes[h] * kLog2e : 0.f;
   const int2 range = sm_range<SS, false>(a, m, b, i0, sh);
-  sm_tile<T, D>(Qs, Q, a.q.t, i0, a.nq, nullptr);
+  sm_tile<D>(Qs, Q, a.q.t, i0, a.nq, nullptr);
   f32x2 acc[4][D / 32];
   float mx[4], sum[4];
   int lim[4], doc[4];
@@ -124,8 +124,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __g
   for (int t = range.x; t < range.y; ++t) {
     const int j0 = t * SS;
     __syncthreads();
-    sm_tile<T, D>(Ks, K, a.k.t, j0, m.len, dk);
-    sm_tile<T, D>(Vs, V, a.v.t, j0, m.len, dk);
+    sm_tile<D>(Ks, K, a.k.t, j0, m.len, dk);
+    sm_tile<D>(Vs, V, a.v.t, j0, m.len, dk);
     __syncthreads();
     float s[4][4] = {};
     sm_dots<D>(Qs, Ks, ty, tx, s);
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __g
     __syncthreads();
     sm_add<D>(Ps, Vs, ty, tx, acc);
   }
-  T* O = static_cast<T*>(a.o.p) + b * a.o.b + h * a.o.h;
+  float* O = static_cast<float*>(a.o.p) + b * a.o.b + h * a.o.h;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
 #pragma unroll
@@ -171,8 +171,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __g
     for (int q = 0; q < D / 32; ++q) {
       float u, v;
       unpack2(mul2(acc[k][q], pack2(inv, inv)), u, v);
-      O[i * a.o.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
-      O[i * a.o.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+      O[i * a.o.t + ColMap<D>::col(tx, 2 * q)] = u;
+      O[i * a.o.t + ColMap<D>::col(tx, 2 * q + 1)] = v;
     }
     if (tx == 0) a.lse[(long long)blockIdx.x * a.nq + i] = sum[k] == 0.f ? -INFINITY : mx[k] * kLn2 + logf(sum[k]);
   }
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_fwd(const __g
 
 // KEYS false: stationary queries (X1 = Q, X2 = dO), moving keys (Y1 = K, Y2 = V): dQ, and delta for the other pass.
 // KEYS true: stationary keys (X1 = K, X2 = V), moving queries (Y1 = Q, Y2 = dO) of every query head of the group: dK, dV.
-template <typename T, int D, bool KEYS>
+template <int D, bool KEYS>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __grid_constant__ SmArgs a) {
   pdl_wait();
   extern __shared__ __align__(16) float sm_smem[];
@@ -194,19 +194,19 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __g
   const int* dq = a.doc_q ? a.doc_q + (long long)b * a.nq : nullptr;
   const int* dk = a.doc_k ? a.doc_k + (long long)b * a.nk : nullptr;
   const int2 range = sm_range<SS, KEYS>(a, m, b, s0, sh);
-  auto slab = [&](const SmView& v, int h) { return static_cast<const T*>(v.p) + b * v.b + h * v.h; };
+  auto slab = [&](const SmView& v, int h) { return static_cast<const float*>(v.p) + b * v.b + h * v.h; };
   if (KEYS) {
-    sm_tile<T, D>(X1, slab(a.k, hs), a.k.t, s0, m.len, dk);
-    sm_tile<T, D>(X2, slab(a.v, hs), a.v.t, s0, m.len, dk);
+    sm_tile<D>(X1, slab(a.k, hs), a.k.t, s0, m.len, dk);
+    sm_tile<D>(X2, slab(a.v, hs), a.v.t, s0, m.len, dk);
   } else {
-    sm_tile<T, D>(X1, slab(a.q, hs), a.q.t, s0, a.nq, dq);
-    sm_tile<T, D>(X2, slab(a.dout, hs), a.dout.t, s0, a.nq, dq);
+    sm_tile<D>(X1, slab(a.q, hs), a.q.t, s0, a.nq, dq);
+    sm_tile<D>(X2, slab(a.dout, hs), a.dout.t, s0, a.nq, dq);
     // delta: row r = tid / 4, a quarter of the channels each
     const int r = tid >> 2, i = s0 + r;
     float v = 0.f;
     if (i < a.nq && !(dq && dq[i] < 0)) {
-      const T* o = slab(a.o, hs) + (long long)i * a.o.t;
-      const T* g = slab(a.dout, hs) + (long long)i * a.dout.t;
+      const float* o = slab(a.o, hs) + (long long)i * a.o.t;
+      const float* g = slab(a.dout, hs) + (long long)i * a.dout.t;
       for (int c = (tid & 3) * (D / 4); c < ((tid & 3) + 1) * (D / 4); c += 4) {
         const float4 x = ld4(o + c), y = ld4(g + c);
         v += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
@@ -232,16 +232,16 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __g
       const int m0 = t * SS;
       __syncthreads();
       if (KEYS) {
-        sm_tile<T, D>(Y1, slab(a.q, h), a.q.t, m0, a.nq, dq);
-        sm_tile<T, D>(Y2, slab(a.dout, h), a.dout.t, m0, a.nq, dq);
+        sm_tile<D>(Y1, slab(a.q, h), a.q.t, m0, a.nq, dq);
+        sm_tile<D>(Y2, slab(a.dout, h), a.dout.t, m0, a.nq, dq);
         if (tid < SS) {
           const long long at = ((long long)b * a.Hq + h) * a.nq + m0 + tid;
           L[tid] = m0 + tid < a.nq ? a.lse[at] * kLog2e : 0.f;
           Dl[tid] = m0 + tid < a.nq ? a.delta[at] : 0.f;
         }
       } else {
-        sm_tile<T, D>(Y1, slab(a.k, hk), a.k.t, m0, m.len, dk);
-        sm_tile<T, D>(Y2, slab(a.v, hk), a.v.t, m0, m.len, dk);
+        sm_tile<D>(Y1, slab(a.k, hk), a.k.t, m0, m.len, dk);
+        sm_tile<D>(Y2, slab(a.v, hk), a.v.t, m0, m.len, dk);
       }
       __syncthreads();
       float s[4][4] = {}, g[4][4] = {};
@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __g
     }
   }
   const SmView& o2 = KEYS ? a.dk : a.dq;
-  T* g2 = static_cast<T*>(o2.p) + b * o2.b + hs * o2.h;
-  T* g1 = KEYS ? static_cast<T*>(a.dv.p) + b * a.dv.b + hs * a.dv.h : nullptr;
+  float* g2 = static_cast<float*>(o2.p) + b * o2.b + hs * o2.h;
+  float* g1 = KEYS ? static_cast<float*>(a.dv.p) + b * a.dv.b + hs * a.dv.h : nullptr;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int i = s0 + ty * 4 + k;
@@ -279,12 +279,12 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) k_softmax_bwd(const __g
     for (int q = 0; q < D / 32; ++q) {
       float u, v;
       unpack2(a2[k][q], u, v);
-      g2[i * o2.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
-      g2[i * o2.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+      g2[i * o2.t + ColMap<D>::col(tx, 2 * q)] = u;
+      g2[i * o2.t + ColMap<D>::col(tx, 2 * q + 1)] = v;
       if (KEYS) {
         unpack2(a1[k][q], u, v);
-        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q)] = from_f<T>(u);
-        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q + 1)] = from_f<T>(v);
+        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q)] = u;
+        g1[i * a.dv.t + ColMap<D>::col(tx, 2 * q + 1)] = v;
       }
     }
   }
