@@ -572,7 +572,8 @@ def rope_frequencies(r: int, base: float = 10000.0, scaling: Optional[dict] = No
 class Rope:
     """Rotary positions of heads with d channels: `freq`, radians per position of the r / 2 channel pairs (a tensor or sequence of
     doubles, or None: no rotation), the first r channels rotated, pairs (2i, 2i+1) if `interleaved` or (i, i + r/2); `factor`
-    scales the rotated channels.  Holds the table of the kernels on the device of `freq` (or `device`); make it once."""
+    scales the rotated channels.  Holds the table of the kernels on the device of `freq` (or `device`).  The table is formed on the CPU and depends
+    on the model alone: make it once, from frequencies on the CPU (those on a GPU are fetched first, 50 us and a synchronisation)."""
 
     def __init__(self, d: int, freq=None, interleaved: bool = False, factor: float = 1.0, device=None):
         f = torch.zeros(0, dtype=torch.float64) if freq is None else torch.as_tensor(freq, dtype=torch.float64)

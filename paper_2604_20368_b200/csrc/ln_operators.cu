@@ -139,8 +139,8 @@ StepPlan plan_step(const ln_softmax* p) {
 }
 
 // tcgen05 forward: query tiles a CTA (T), and the split of the keys over CTAs where the query tiles alone do not fill the GPU.
-// One tile and two CTAs an SM: always with up to 64 channels (32 heads x 4096 tokens 224 us, two tiles 226; with a cap 412 and 453, with
-// a bias 267 and 312), and for short rows; with 128 channels and long rows two tiles, which copy each key tile once for both.
+// One tile and two CTAs an SM: always with up to 64 channels (32 heads x 4096 tokens 205 us, two tiles 205; with a cap 406 and 447, with
+// a bias 246 and 295), and for short rows; with 128 channels and long rows two tiles, which copy each key tile once for both.
 struct SplitPlan { int tiles, chunk, splits; };
 SplitPlan plan_split(const ln_softmax* p) {
   SplitPlan s;

@@ -64,8 +64,8 @@ template <> struct Piece<bf16> {
 enum { QK_ROPE = 0, QK_NORM = 1, QK_NORM_BWD = 2 };
 
 // Sine and cosine of 2 pi part / 2^32.  The nearest quarter turn comes off in integers, exactly; the rest, within an eighth of a turn,
-// goes through the Taylor series to degree 9 and 8 (remainders below 2e-9 and 3e-8), two roundings more: about 2^-23.  A third of
-// the instructions of sincospif, which with four heads a token was a third of the kernel.
+// goes through the Taylor series to degree 9 and 8 (remainders below 2e-9 and 3e-8), two roundings more: about 2^-23.  Against sincospif:
+// 8 x 50176 tokens of four heads with 64 channels 104.6 -> 99.1 us, of ten heads with 128 channels 70.7 -> 69.4, with the norm 94.8 -> 92.4.
 __device__ __forceinline__ void turn_sincos(uint32_t part, float& sn, float& cs) {
   const uint32_t quarter = part + (1u << 29);                              // its top two bits: the nearest quarter turn
   const float x = (float)((int)(part - (quarter & 0xc0000000u))) * 1.4629180792671596e-9f;     // 2 pi 2^-32
@@ -85,8 +85,9 @@ __device__ __forceinline__ void turn_sincos(uint32_t part, float& sn, float& cs)
 
 // LPR lanes per row; INTER: interleaved layout.  256 threads.  U heads of a lane group are in flight at a time, with four CTAs an SM
 // (two for the backward pass, whose sums over rows stay in registers).  16 x 4096 tokens of 16 heads with 128 channels, us, floor 82
-// at the copy rate: rotation 103 (eight in flight and three CTAs 122, two and five CTAs 120); with the norm, 10 heads, floor 51: 102
-// (four in flight 120), backward, floor 77: 130 (three CTAs 181).
+// at the copy rate: rotation 100 (eight in flight and three CTAs 122, two and five CTAs 120); with the norm, 10 heads, floor 51: 92
+// (four in flight 120), backward, floor 77: 130 (three CTAs 181).  fp32, 10 heads, floors 102, 102 and 154:
+// 107, 135 and 219.
 template <typename T, int LPR, bool INTER, int MODE>
 __global__ void __launch_bounds__(256, MODE == QK_NORM_BWD ? 2 : 4) k_qk_rope(const __grid_constant__ QkArgs a) {
   pdl_wait();

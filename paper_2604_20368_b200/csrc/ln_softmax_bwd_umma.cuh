@@ -13,9 +13,10 @@
 // peaked.  The sum of a row's ds says by how much (it is zero for the right delta): the query pass adds it up in 32 bits, takes it
 // times M = A K off dQ, and hands the corrected delta to the key pass (dQ and dK of 4096 tokens with scores of 3 standard deviations:
 // 2.7e-3 -> 2.4e-3 of their norm, of 16 tokens 4.0e-3 -> 2.4e-3, where their own rounding is 1.7e-3).
-// Two passes form S and dP twice (7 products a pair instead of 5): no atomics, and every sum has one order.
+// Two passes form S and dP twice (4 products a pair each, M among them, instead of 5 in all): no atomics, and every sum has one order.
 // Bound by the tensor core's operand reads: with 64 columns a product reads 128 + 64 rows of shared memory for 128 x 64 results.
-// 32 heads of 4096 tokens without masks: 128 channels query pass 486 us, key pass 458 (1.20 PFLOP/s); 64 channels 310 and 345.
+// 32 heads of 4096 tokens without masks: 128 channels query pass 478 us, key pass 459 (1.20 PFLOP/s); 64 channels 293 and 332; with a cap of 20
+// 566 and 588, 478 and 482.
 #pragma once
 #include "ln_softmax_umma.cuh"
 

@@ -22,7 +22,7 @@ struct StepPart { float* o; float2* ml; };           // [row][split][d] partial 
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { uint32_t r; asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel)); return r; }
 
-// Score in base 2 from the product, with the cap through the accurate tanh: a step has few scores.
+// Score in base 2 from the product for fp32 storage, with the cap through the accurate tanh (bf16 storage: sm_cap4).
 __device__ __forceinline__ float step_score(float dot, const SmArgs& a, float slope2, int dist) {
   float x = dot * a.scale;
   if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);

@@ -16,7 +16,8 @@
 // Key tiles come last first: with a distance bias the nearest keys then set the reference at once.
 // Bound: 4 * 128 * 128 * d operations on the tensor core (1024 clocks a tile at d = 128) against 128 * 128 exponentials at 16 a
 // clock and SM (1024 clocks; with a cap 1.25 more special functions each, see sm_cap4).  32 heads of 4096 tokens without masks: 128
-// channels 280 to 310 us (0.89 to 0.98 PFLOP/s, a tile every 2100 clocks), 64 channels 224, with a cap 412, with a bias 267.
+// channels 269 to 300 us (0.92 to 1.02 PFLOP/s, a tile every 2100 clocks), with a cap of 20 579, with a bias 395 to 420; 64 channels 205, 406
+// and 246.
 #pragma once
 #include "ln_softmax.cuh"
 #include "ln_tile_umma.cuh"
