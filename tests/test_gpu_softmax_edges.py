@@ -188,3 +188,20 @@ def test_gradients_of_peaked_rows_are_as_good_as_their_roundings(n, sigma, cap):
         err = float((got[k].cpu().double() - val[k]).norm() / val[k].norm())
         print(k, err)
         assert err < bound, (k, err)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("nq", [2, 140])
+def test_overlapping_rows_and_a_bias_that_grows_with_distance(dtype, nq):
+    """Windows over one buffer, a row eight elements behind the last; negative slopes, so that the farthest key weighs most and A of the
+    nearest lies below 2^-126."""
+    nk, d = 300, 64
+    g = torch.Generator().manual_seed(4)
+    windows = lambda n: torch.randn(2, 2, n * 8 + d, generator=g).to(dtype).to(DEV).as_strided((2, 2, n, d), (2 * (n * 8 + d), n * 8 + d, 8, 1))
+    Q, K, V, dO = windows(nq), windows(nk), windows(nk), windows(nq)
+    kw = dict(causal=True, slopes=torch.tensor([-0.3, -0.01]))
+    got = _run(Q, K, V, dO, **kw)
+    val, tol = attention(Q, K, V, dO, dtype=dtype, **kw)
+    for k, t in _underflow(Q, K, V, dO).items():
+        tol[k] += t
+    print(check(got, val, tol))
